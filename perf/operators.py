@@ -196,7 +196,7 @@ def _encode(x):
     b = x.float().unflatten(-1, (-1, BLOCK))
     top = b.abs().amax(-1)
     bits = top.view(torch.int32)
-    e = torch.clamp((bits >> 23) - 2 + ((bits & 0x7FFFFF) > 0x400000).int(), min=1)
+    e = torch.clamp((bits >> 23) - 2 + ((bits & 0x7FFFFF) > 0x400000).int(), min=1, max=252)
     e = torch.where(torch.isfinite(top), e, torch.full_like(e, 255))
     y = b * ((254 - e.clamp(max=253)) << 23).view(torch.float32).unsqueeze(-1)
     m = y.abs()
@@ -572,11 +572,11 @@ def _grid64(x):
     b = x.double().unflatten(-1, (-1, BLOCK))
     top = b.abs().amax(-1, keepdim=True)
     _, e = torch.frexp(top / 6.0)                       # top / 6 = f 2^e, 0.5 <= f < 1
-    e = torch.where(_power64(e - 1) * 6.0 >= top, e - 1, e).clamp(min=-126)
+    e = torch.where(_power64(e - 1) * 6.0 >= top, e - 1, e).clamp(min=-126, max=125)
     unit = _power64(e)
     y = b / unit
     step = torch.where(y.abs() < 2, 0.5, torch.where(y.abs() < 4, 1.0, 2.0)).double()
-    return (torch.round(y / step) * step * unit).flatten(-2)
+    return ((torch.round(y / step) * step).clamp(-6, 6) * unit).flatten(-2)
 
 
 def _draft64(st):
