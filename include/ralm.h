@@ -16,6 +16,12 @@
  * (ralm_os3_*), and for KNN-LM datastores (Section 5.3) ranking by distance
  * (RALM_METRIC_L2) and the neighbour distribution (ralm_knnlm_probs).
  *
+ * For the generator that runs next to the loop, on the card that the datastore
+ * shares: a paged cache of keys and values in 4 bits, attention over it, the
+ * forking, rolling back and compacting of its pages (ralm_kv_*), and the
+ * verification of drafted tokens against a target's probabilities
+ * (ralm_verify_draft).
+ *
  * General conventions
  *   - Unless a parameter says "host", every data pointer is a DEVICE pointer
  *     owned by the caller.  The library keeps no reference after the call's
@@ -39,7 +45,7 @@
  *     formed in double from fp32 (or exactly widened fp16/bf16) inputs.
  *   - Argument errors are detected on the host before anything is launched and
  *     are reported as a status; ralm_last_error() gives the text.  Inputs are
- *     assumed finite (NaN/Inf: behaviour unspecified).
+ *     assumed finite (NaN/Inf: behaviour unspecified) where nothing else is said.
  */
 #ifndef RALM_H
 #define RALM_H
@@ -494,6 +500,180 @@ ralm_status ralm_knnlm_probs(const int32_t *ids, const float *scores, int64_t Q,
                              const int32_t *values, int64_t N, float temperature, int32_t *out_tokens,
                              float *out_weights, int32_t *out_top_token, float *out_top_prob,
                              void *stream);
+
+/*
+ * The generator's cache of keys and values, in 4 bits and in pages.
+ *
+ * A request's tokens lie in pages of page_tokens tokens; a page holds them for
+ * all layers and heads, so that forking, rolling back and copying a context is
+ * one operation for all layers.  Which pages are whose:
+ *
+ *   table  device int32 [R, max_pages]: the page of the request's tokens
+ *          page_tokens * j .. ; -1 behind its last page
+ *   lens   device int32 [R]: tokens of the request
+ *   refs   device int32 [n_pages]: how many places of the table hold the page;
+ *          0 = free (append, read, attention and copy_pages do not use it: NULL)
+ *   pages  device, n_pages * ralm_kv_page_bytes() bytes, 16-byte aligned
+ *
+ * A new cache is lens = refs = 0 and table = -1; its pages need no clearing.
+ * d is 64, 128 or 256; page_tokens a power of two in [16, 256]; n_pages <=
+ * 2^22, R <= 2^16, max_pages * page_tokens <= 2^30.
+ *
+ * Format: 32 neighbouring numbers of a head share a power of two 2^e, stored as
+ * e + 127 in a byte, and each is one of +-{0, .5, 1, 1.5, 2, 3, 4, 6} * 2^e: 4.25
+ * bits a number.  e is the smallest integer in [-126, 125] with max|x| <= 6 * 2^e
+ * (125 beyond 6 * 2^125, so that what is finite stays so in fp32 and bf16), a number
+ * becomes the nearest of the sixteen, ties to the even code (0, 1, 2, 4).
+ * A block that holds an infinity or NaN gets the byte 255 and stands for NaN.
+ * fp32, bf16 and fp16 inputs of equal value give equal codes.  (Layout of a page:
+ * [layer][head][page_tokens / 16][17 d] bytes; kv_kernels.h has the rest.)
+ *
+ * Table entries outside [0, n_pages) are no places: tokens there are not stored,
+ * read as zeros and not attended to.  Pages of one request must be distinct, and
+ * a page that another request shares must not be appended to: ralm_kv_reserve
+ * sees to both.
+ */
+typedef struct {
+    void *pages;
+    int64_t n_pages;
+    int32_t n_layers, n_heads, d, page_tokens;
+    int32_t *table;
+    int32_t *lens;
+    int32_t *refs;
+    int64_t R;
+    int32_t max_pages;
+} ralm_kv_t;
+
+/* Bytes of a page; 0 for arguments out of range. */
+size_t ralm_kv_page_bytes(int32_t n_layers, int32_t n_heads, int32_t d, int32_t page_tokens);
+
+/*
+ * Keys and values of new tokens into the cache of a layer, and out of it.
+ *
+ *   k, v       device [n, n_heads, d] of dtype (fp32, bf16 or fp16); strides in
+ *              elements from token to token and head to head (0: dense);
+ *              bases and strides multiples of 16 bytes
+ *   offsets    device int64 [R+1], non-decreasing: rows offsets[r] ..
+ *              offsets[r+1]-1 are request r's
+ *   append     they are the request's last tokens: row i of s goes to place
+ *              lens[r] - s + i (ralm_kv_reserve has made the room and moved lens)
+ *   read       from place start[r] on (device int32 [R]), or the last ones too
+ *              (start == NULL).  fp16 overflows to infinity beyond its range.
+ *
+ * Rows of no request are neither stored nor written; places outside the table
+ * are not stored and read as zeros.
+ */
+ralm_status ralm_kv_append(const ralm_kv_t *kv, int32_t layer, const void *k, const void *v, int32_t dtype,
+                           int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                           int64_t v_head_stride, const int64_t *offsets, int64_t n, void *stream);
+ralm_status ralm_kv_read(const ralm_kv_t *kv, int32_t layer, const int64_t *offsets, int64_t n,
+                         const int32_t *start, void *k, void *v, int32_t dtype, int64_t k_token_stride,
+                         int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                         void *stream);
+
+/*
+ * Attention of every request's last tokens over its cache:
+ *
+ *   out[i, h] = sum_j softmax_j(scale * q[i, h] . K[j, h / G]) V[j, h / G],   G = n_q_heads / n_heads
+ *
+ * over the tokens j that query i sees.  The s_r = offsets[r+1] - offsets[r]
+ * queries of request r stand at its last places p = lens[r] - s_r + i, their own
+ * keys and values having been appended; they see j <= p, and with window > 0 of
+ * those only j > p - window and the first `sinks` tokens.  One token per request,
+ * drafted tokens and chunks of a prompt are the same call.
+ *
+ *   q, out     device [Qt, n_q_heads, d], bf16 or fp16; strides in elements
+ *              (0: dense), multiples of 8; bases 16-byte aligned
+ *   max_q, max_len  the largest s_r and lens[r], as far as the host knows them
+ *              (0: Qt, the table's width): they choose the launch.  Smaller than
+ *              the truth they cost time, never a result.
+ *   lse        device fp32 [Qt, n_q_heads] or NULL: log sum exp of a row's scores
+ *   workspace  ralm_kv_attention_workspace_bytes(), 16-byte aligned (may be NULL
+ *              where that is 256): sums of contexts that are split over workgroups
+ *
+ * A row that sees nothing (lens[r] < s_r) is 0, its lse -inf.  Scores and sums
+ * are fp32; weights are rounded to 8 bits (bf16) or 16 bits (fp16) for their
+ * product with V.  A key that is NaN makes the rows that see it NaN, a value the
+ * 32 numbers of its block; rows that do not see it are not touched.  Results are
+ * the same from call to call.
+ */
+size_t ralm_kv_attention_workspace_bytes(const ralm_kv_t *kv, int32_t n_q_heads, int64_t Qt, int64_t max_q,
+                                         int64_t max_len, int32_t window, int32_t sinks);
+ralm_status ralm_kv_attention(const ralm_kv_t *kv, int32_t layer, const void *q, int32_t dtype,
+                              int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
+                              const int64_t *offsets, int64_t Qt, int64_t max_q, int64_t max_len, float scale,
+                              int32_t window, int32_t sinks, void *out, int64_t out_token_stride,
+                              int64_t out_head_stride, float *lse, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/*
+ * Pages.  The free page that is taken is always the one with the lowest id, so
+ * the state behind a call follows from the state before it.  All of them work on
+ * kv's table, lens and refs in place, on the device, without the host knowing
+ * any length.  Workspace: ralm_kv_pages_workspace_bytes(), 16-byte aligned.
+ *
+ * ralm_kv_reserve  room for grow[r] more tokens (device int32 [R]; <= 0: none) of
+ *   every request, lens[r] += grow[r].  New pages are taken in the order of the
+ *   requests; a last page that is partly filled and shared (its count above 1
+ *   when the call begins) is copied to a page of the request's own first.  A
+ *   request is served if the pages needed up to and with it are there (or it
+ *   needs none); others, and those that would outgrow the table, stay as they are.
+ *   granted: device int32 [R] or NULL, 1 or 0.
+ * ralm_kv_fork  for i < n: request dst[i], which must be empty, shares the pages
+ *   of src[i]'s first keep[i] tokens (keep NULL: all).  Pairs whose dst is not
+ *   empty or whose ids are out of range or equal are left out; a dst comes once in
+ *   a call and is no src of it.
+ * ralm_kv_truncate  lens[r] = min(lens[r], new_lens[r]); pages behind it are let
+ *   go, and free when nobody else holds them.  0 ends a request; the
+ *   first_mismatch of a verification rolls it back.
+ * ralm_kv_copy_pages  contents of page src[i] to page dst[i], i < n; no dst may be
+ *   a src or come twice.  Ids out of range are left out.
+ * ralm_kv_compact  the n pages in use become pages 0 .. n-1: those at n and behind,
+ *   in order, take the free places in front, in order.  The new table, counts and n
+ *   go to table_out [R, max_pages], refs_out [n_pages], used [1]; they may be the
+ *   cache's own.  If they are not, the old table stays valid (nothing of what it
+ *   names is overwritten) until the new counts are used to reserve.
+ */
+size_t ralm_kv_pages_workspace_bytes(const ralm_kv_t *kv);
+ralm_status ralm_kv_reserve(const ralm_kv_t *kv, const int32_t *grow, int32_t *granted, void *workspace,
+                            size_t workspace_bytes, void *stream);
+ralm_status ralm_kv_fork(const ralm_kv_t *kv, const int32_t *src, const int32_t *dst, const int32_t *keep,
+                         int64_t n, void *stream);
+ralm_status ralm_kv_truncate(const ralm_kv_t *kv, const int32_t *new_lens, void *stream);
+ralm_status ralm_kv_copy_pages(const ralm_kv_t *kv, const int32_t *src, const int32_t *dst, int64_t n, void *stream);
+ralm_status ralm_kv_compact(const ralm_kv_t *kv, int32_t *table_out, int32_t *refs_out, int32_t *used,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Verification of drafted tokens by a target's probabilities (the sampled form
+ * of ralm_verify's compare: the tokens that come out are distributed as the
+ * target's own).  Request r drafted s_r = q_offsets[r+1] - q_offsets[r] tokens.
+ *
+ *   draft_ids     device int32 [Qt]
+ *   draft_probs   device [Qt, V], what they were drawn from; NULL: every draft is
+ *                 certain (a greedy draft, a neighbour's token)
+ *   target_probs  device [Qt + R, V]: row q_offsets[r] + r + i belongs to the i-th
+ *                 draft of request r, row i = s_r to the token behind them
+ *   *_stride      elements from row to row (0 = V); dtype fp32, bf16 or fp16 for both
+ *   u [Qt], u_next [R]  device fp32, uniform in [0, 1)
+ *   accepted      device int32 [R]: the first i with u_i q_i(x_i) >= p_i(x_i), or s_r
+ *   next_token    device int32 [R]: drawn by u_next from max(p - q, 0) of that row (from
+ *                 p if nothing is left, or behind s_r accepted ones); -1 if p is 0 too
+ *   workspace     ralm_verify_draft_workspace_bytes(), 16-byte aligned
+ *
+ * Defined in whole numbers, so that it does not depend on how sums are formed: P =
+ * floor(min(max(p, 0), 1) * 2^36), Q alike, m = floor(u * 2^24); accepted while
+ * m Q < 2^24 P; w = max(P - Q, 0), S = sum w; the next token is the smallest v with
+ * w_0 + .. + w_v > floor(m S / 2^24).  NaN counts as 0, a draft outside [0, V) is not accepted.
+ * R <= 2^16, V <= RALM_MAX_VOCABULARY.
+ */
+#define RALM_MAX_VOCABULARY (1 << 20)
+size_t ralm_verify_draft_workspace_bytes(int64_t R, int32_t V);
+ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs, int64_t draft_stride,
+                              const void *target_probs, int64_t target_stride, int32_t dtype, int32_t V,
+                              const float *u, const float *u_next, int64_t Qt, const int64_t *q_offsets,
+                              int64_t R, int32_t *accepted, int32_t *next_token, void *workspace,
+                              size_t workspace_bytes, void *stream);
 
 /*
  * Optimal speculation stride scheduler, OS^3 (Section 4; estimation of its

@@ -33,6 +33,13 @@ class ralm_datastore_t(ctypes.Structure):
                 ("metric", ctypes.c_int32)]
 
 
+class ralm_kv_t(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("d", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("R", ctypes.c_int64), ("max_pages", ctypes.c_int32)]
+
+
 class ralm_counters_t(ctypes.Structure):
     _fields_ = [("unanswered", ctypes.c_int32), ("ladder_overflows", ctypes.c_int32),
                 ("hard_certified", ctypes.c_int32), ("soft_certified", ctypes.c_int32),
@@ -101,6 +108,27 @@ def lib() -> ctypes.CDLL:
         L.ralm_profile_enable.argtypes = [i32]
         L.ralm_profile_enable.restype = None
         L.ralm_profile_scan_ms.argtypes = [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(i32)]
+        kvp, size = ctypes.POINTER(ralm_kv_t), ctypes.c_size_t
+        L.ralm_kv_page_bytes.argtypes = [i32, i32, i32, i32]
+        L.ralm_kv_append.argtypes = [kvp, i32, vp, vp, i32, i64, i64, i64, i64, vp, i64, vp]
+        L.ralm_kv_read.argtypes = [kvp, i32, vp, i64, vp, vp, vp, i32, i64, i64, i64, i64, vp]
+        L.ralm_kv_attention_workspace_bytes.argtypes = [kvp, i32, i64, i64, i64, i32, i32]
+        L.ralm_kv_attention.argtypes = [kvp, i32, vp, i32, i64, i64, i32, vp, i64, i64, i64, ctypes.c_float, i32, i32, vp, i64, i64,
+                                        vp, vp, size, vp]
+        L.ralm_kv_pages_workspace_bytes.argtypes = [kvp]
+        L.ralm_kv_reserve.argtypes = [kvp, vp, vp, vp, size, vp]
+        L.ralm_kv_fork.argtypes = [kvp, vp, vp, vp, i64, vp]
+        L.ralm_kv_truncate.argtypes = [kvp, vp, vp]
+        L.ralm_kv_copy_pages.argtypes = [kvp, vp, vp, i64, vp]
+        L.ralm_kv_compact.argtypes = [kvp, vp, vp, vp, vp, size, vp]
+        L.ralm_verify_draft_workspace_bytes.argtypes = [i64, i32]
+        L.ralm_verify_draft.argtypes = [vp, vp, i64, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, size, vp]
+        for name in ("ralm_kv_page_bytes", "ralm_kv_attention_workspace_bytes", "ralm_kv_pages_workspace_bytes",
+                     "ralm_verify_draft_workspace_bytes"):
+            getattr(L, name).restype = size
+        for name in ("ralm_kv_append", "ralm_kv_read", "ralm_kv_attention", "ralm_kv_reserve", "ralm_kv_fork", "ralm_kv_truncate",
+                     "ralm_kv_copy_pages", "ralm_kv_compact", "ralm_verify_draft"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("ralm_retrieve_topk", "ralm_retrieve_topk_ex", "ralm_retrieve_topk_seq", "ralm_workspace_overflows",
                      "ralm_workspace_counters", "ralm_workspace_stage_entries", "ralm_scan_routes", "ralm_first_stage_scores",
                      "ralm_build_scan_copy", "ralm_build_scan_copy_l2", "ralm_cache_lookup", "ralm_cache_lookup_all",
@@ -403,6 +431,177 @@ def ralm_knnlm_probs(ids: torch.Tensor, scores: torch.Tensor, values: torch.Tens
                                   float(temperature), tokens.data_ptr(), weights.data_ptr(), _ptr(top_token),
                                   _ptr(top_prob), _stream()))
     return tokens, weights, top_token, top_prob
+
+
+class KVCache:
+    """A paged cache of keys and values in 4 bits: the caller's tensors and the descriptor that the calls take.
+
+    ``pages`` uint8 (n_pages rows of ``ralm_kv_page_bytes`` bytes, or flat), ``table`` int32 [R, max_pages], ``lens`` int32 [R],
+    ``refs`` int32 [n_pages]."""
+
+    def __init__(self, pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, *, n_layers: int,
+                 n_heads: int, d: int, page_tokens: int):
+        for t in (table, lens, refs):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        assert pages.dtype == torch.uint8 and pages.is_contiguous() and table.dim() == 2 and lens.shape == table.shape[:1]
+        page = ralm_kv_page_bytes(n_layers, n_heads, d, page_tokens)
+        assert pages.numel() == refs.numel() * page, "pages must hold refs.numel() pages"
+        self.pages, self.table, self.lens, self.refs = pages, table, lens, refs
+        self.n_layers, self.n_heads, self.d, self.page_tokens = n_layers, n_heads, d, page_tokens
+        self.desc = ralm_kv_t(pages.data_ptr(), refs.numel(), n_layers, n_heads, d, page_tokens, table.data_ptr(), lens.data_ptr(),
+                              refs.data_ptr(), table.shape[0], table.shape[1])
+
+    @classmethod
+    def empty(cls, R: int, max_tokens: int, n_pages: int, *, n_layers: int, n_heads: int, d: int, page_tokens: int = 32,
+              device="cuda") -> "KVCache":
+        """A cache without tokens: R requests of up to max_tokens tokens in n_pages pages."""
+        page = ralm_kv_page_bytes(n_layers, n_heads, d, page_tokens)
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.empty(n_pages, page, dtype=torch.uint8, device=device),
+                   torch.full((R, -(-max_tokens // page_tokens)), -1, **i32), torch.zeros(R, **i32), torch.zeros(n_pages, **i32),
+                   n_layers=n_layers, n_heads=n_heads, d=d, page_tokens=page_tokens)
+
+
+def ralm_kv_page_bytes(n_layers: int, n_heads: int, d: int, page_tokens: int) -> int:
+    n = lib().ralm_kv_page_bytes(n_layers, n_heads, d, page_tokens)
+    if n == 0:
+        raise RalmError(2, "ralm_kv_page_bytes: bad arguments")
+    return int(n)
+
+
+def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor):
+    assert k.shape == v.shape and k.dim() == 3 and k.shape[1:] == (kv.n_heads, kv.d) and k.dtype == v.dtype
+    assert k.stride(2) == 1 and v.stride(2) == 1
+    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape[0] == kv.lens.shape[0] + 1
+    return k.stride(0), k.stride(1), v.stride(0), v.stride(1)
+
+
+def ralm_kv_append(kv: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor) -> None:
+    """``k``, ``v`` [n, n_heads, d]: the last tokens of every request (room for them has been reserved)."""
+    st = _kv_rows(kv, k, v, offsets)
+    _check(lib().ralm_kv_append(ctypes.byref(kv.desc), layer, k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, offsets.data_ptr(),
+                                k.shape[0], _stream()))
+
+
+def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: Optional[torch.Tensor] = None,
+                 dtype: torch.dtype = torch.bfloat16, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None
+                 ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values [n, n_heads, d] of every request's last tokens, or of those from ``start`` (int32 [R]) on."""
+    if k is None:
+        k = torch.empty(n, kv.n_heads, kv.d, dtype=dtype, device=kv.pages.device)
+    if v is None:
+        v = torch.empty(n, kv.n_heads, kv.d, dtype=k.dtype, device=kv.pages.device)
+    st = _kv_rows(kv, k, v, offsets)
+    assert k.shape[0] == n and (start is None or (start.dtype == torch.int32 and start.shape == kv.lens.shape))
+    _check(lib().ralm_kv_read(ctypes.byref(kv.desc), layer, offsets.data_ptr(), n, _ptr(start), k.data_ptr(), v.data_ptr(),
+                              _DT[k.dtype], *st, _stream()))
+    return k, v
+
+
+def alloc_kv_attention_workspace(kv: KVCache, n_q_heads: int, Qt: int, max_q: int = 0, max_len: int = 0, window: int = 0,
+                                 sinks: int = 0) -> torch.Tensor:
+    n = lib().ralm_kv_attention_workspace_bytes(ctypes.byref(kv.desc), n_q_heads, Qt, max_q, max_len, window, sinks)
+    if n == 0:
+        raise RalmError(2, lib().ralm_last_error().decode())
+    return torch.empty(int(n), dtype=torch.uint8, device=kv.pages.device)
+
+
+def ralm_kv_attention(kv: KVCache, layer: int, q: torch.Tensor, offsets: torch.Tensor, max_q: int = 0, max_len: int = 0,
+                      scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of every request's last tokens (``q`` [Qt, heads, d]) over its cache; ``scale`` None: d ** -0.5."""
+    assert q.dim() == 3 and q.shape[2] == kv.d and q.stride(2) == 1
+    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape[0] == kv.lens.shape[0] + 1
+    Qt, heads, d = q.shape
+    if out is None:
+        out = torch.empty(Qt, heads, d, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous())
+    if q.dtype not in _DT:
+        raise RalmError(4, f"dtype {q.dtype}")
+    if workspace is None:
+        workspace = alloc_kv_attention_workspace(kv, heads, Qt, max_q, max_len, window, sinks)
+    _check(lib().ralm_kv_attention(ctypes.byref(kv.desc), layer, q.data_ptr(), _DT[q.dtype], q.stride(0), q.stride(1), heads,
+                                   offsets.data_ptr(), Qt, max_q, max_len, d ** -0.5 if scale is None else float(scale), window, sinks,
+                                   out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), workspace.data_ptr(), workspace.numel(),
+                                   _stream()))
+    return out
+
+
+def alloc_kv_pages_workspace(kv: KVCache) -> torch.Tensor:
+    n = int(lib().ralm_kv_pages_workspace_bytes(ctypes.byref(kv.desc)))
+    return torch.empty(n, dtype=torch.uint8, device=kv.pages.device)
+
+
+def ralm_kv_reserve(kv: KVCache, grow: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                    granted: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Room for ``grow`` (int32 [R]) more tokens; int32 [R]: 1 where there was."""
+    assert grow.dtype == torch.int32 and grow.shape == kv.lens.shape and grow.is_contiguous()
+    if workspace is None:
+        workspace = alloc_kv_pages_workspace(kv)
+    if granted is None:
+        granted = torch.empty_like(grow)
+    assert granted.dtype == torch.int32 and granted.shape == grow.shape and granted.is_contiguous()
+    _check(lib().ralm_kv_reserve(ctypes.byref(kv.desc), grow.data_ptr(), granted.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                 _stream()))
+    return granted
+
+
+def ralm_kv_fork(kv: KVCache, src: torch.Tensor, dst: torch.Tensor, keep: Optional[torch.Tensor] = None) -> None:
+    assert src.dtype == torch.int32 and dst.dtype == torch.int32 and src.shape == dst.shape and src.dim() == 1
+    assert src.is_contiguous() and dst.is_contiguous()
+    assert keep is None or (keep.dtype == torch.int32 and keep.shape == src.shape and keep.is_contiguous())
+    _check(lib().ralm_kv_fork(ctypes.byref(kv.desc), src.data_ptr(), dst.data_ptr(), _ptr(keep), src.shape[0], _stream()))
+
+
+def ralm_kv_truncate(kv: KVCache, new_lens: torch.Tensor) -> None:
+    assert new_lens.dtype == torch.int32 and new_lens.shape == kv.lens.shape and new_lens.is_contiguous()
+    _check(lib().ralm_kv_truncate(ctypes.byref(kv.desc), new_lens.data_ptr(), _stream()))
+
+
+def ralm_kv_copy_pages(kv: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+    assert src.dtype == torch.int32 and dst.dtype == torch.int32 and src.shape == dst.shape and src.dim() == 1
+    assert src.is_contiguous() and dst.is_contiguous()
+    _check(lib().ralm_kv_copy_pages(ctypes.byref(kv.desc), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream()))
+
+
+def ralm_kv_compact(kv: KVCache, table: Optional[torch.Tensor] = None, refs: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(table, refs, number of pages in use [1]) of the cache with its pages brought to the front; pass kv.table and kv.refs to
+    have them in place, or make a KVCache of the new ones."""
+    table = torch.empty_like(kv.table) if table is None else table
+    refs = torch.empty_like(kv.refs) if refs is None else refs
+    assert table.dtype == torch.int32 and table.shape == kv.table.shape and table.is_contiguous()
+    assert refs.dtype == torch.int32 and refs.shape == kv.refs.shape and refs.is_contiguous()
+    used = torch.empty((), dtype=torch.int32, device=table.device)
+    if workspace is None:
+        workspace = alloc_kv_pages_workspace(kv)
+    _check(lib().ralm_kv_compact(ctypes.byref(kv.desc), table.data_ptr(), refs.data_ptr(), used.data_ptr(), workspace.data_ptr(),
+                                 workspace.numel(), _stream()))
+    return table, refs, used
+
+
+def ralm_verify_draft(draft_ids: torch.Tensor, target_probs: torch.Tensor, u: torch.Tensor, u_next: torch.Tensor,
+                      q_offsets: torch.Tensor, draft_probs: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(accepted drafts [R], next token [R]) int32; ``target_probs`` [Qt + R, V], ``draft_probs`` [Qt, V] or None (certain drafts)."""
+    R, Qt = q_offsets.shape[0] - 1, draft_ids.shape[0]
+    V = target_probs.shape[1]
+    assert draft_ids.dtype == torch.int32 and u.dtype == torch.float32 and u_next.dtype == torch.float32
+    assert q_offsets.dtype == torch.int64 and u.shape == (Qt,) and u_next.shape == (R,) and target_probs.shape[0] == Qt + R
+    assert all(t.is_contiguous() for t in (draft_ids, u, u_next, q_offsets)) and target_probs.stride(1) == 1
+    if draft_probs is not None:
+        assert draft_probs.shape == (Qt, V) and draft_probs.dtype == target_probs.dtype and draft_probs.stride(1) == 1
+    dev = target_probs.device
+    if workspace is None:
+        workspace = torch.empty(max(1, int(lib().ralm_verify_draft_workspace_bytes(R, V))), dtype=torch.uint8, device=dev)
+    accepted = torch.empty(R, dtype=torch.int32, device=dev)
+    token = torch.empty(R, dtype=torch.int32, device=dev)
+    _check(lib().ralm_verify_draft(draft_ids.data_ptr(), _ptr(draft_probs), 0 if draft_probs is None else draft_probs.stride(0),
+                                   target_probs.data_ptr(), target_probs.stride(0), _DT[target_probs.dtype], V, u.data_ptr(),
+                                   u_next.data_ptr(), Qt, q_offsets.data_ptr(), R, accepted.data_ptr(), token.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel(), _stream()))
+    return accepted, token
 
 
 def ralm_os3_gamma(strides, matched, gamma_max: float = 0.6) -> float:

@@ -25,6 +25,7 @@
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "ralm_kernels.h"
+#include "kv_kernels.h"
 
 using namespace ralm;
 
@@ -316,6 +317,15 @@ hipEvent_t g_prof_ev[MAX_PROF][2];
 int g_prof_made = 0;
 
 }  // namespace
+
+ralm_status ralm::set_error(ralm_status st, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return st;
+}
 
 extern "C" {
 
