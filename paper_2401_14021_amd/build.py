@@ -24,7 +24,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 
 # Matrix results in vector registers: the kernel fills the accumulation registers with its queries.  An option of the compiler's
 # back end (ROCm 7.2); one that does not know it refuses this file.
-EXTRA = {"scan_held_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {"scan_held_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         # the attention rescales and converts its results: in accumulation registers each would be moved twice a step
+         "kv_attention_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str) -> str:

@@ -227,57 +227,44 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
         const int steps = v1 > v0 ? ((v1 - v0 + 1) / 2 + STRIDE - 1 - (ROWS ? 0 : wave)) / STRIDE : 0;
         const int step0 = ROWS ? 0 : wave;
 
-        // page ids of the wave's next 32 steps, two tiles each, a lane per tile
-        auto ids_of = [&](int k) {
-            const int v = v0 + 2 * (step0 + (k + (lane >> 1)) * STRIDE) + (lane & 1);
-            const int tile = v < sp.sinks ? v : v - sp.sinks + sp.lo;
-            const int slot = tile >> kv.tile_shift;
-            return v < v1 && slot < kv.max_pages ? table[slot] : -1;
-        };
+        // The wave's next 32 steps, two tiles each, a lane per tile: where the tile lies, whether it is there, and whether all of the wave's
+        // rows see all of it.  One look at the table for 1024 tokens, and two instructions per tile to have its address.
+        int64_t tile_at = 0;
+        uint64_t there = 0, plain = 0;
         auto tile_of = [&](int k, int u) {
             const int v = v0 + 2 * (step0 + k * STRIDE) + u;
             return v < sp.sinks ? v : v - sp.sinks + sp.lo;
         };
-        int ids = steps > 0 ? ids_of(0) : -1;
-        auto load_step = [&](int k, Piece<D> (&x)[2], int (&page)[2]) {
+        auto look_up = [&](int k) {
+            const int v = v0 + 2 * (step0 + (k + (lane >> 1)) * STRIDE) + (lane & 1);
+            const int tile = v < sp.sinks ? v : v - sp.sinks + sp.lo;
+            const int slot = tile >> kv.tile_shift;
+            const int id = v < v1 && slot < kv.max_pages ? table[slot] : -1;
+            const bool ok = id >= 0 && id < kv.n_pages;
+            tile_at = (ok ? id : 0) * kv.page_bytes + (tile & tile_mask) * kv_tile_bytes(D);
+            there = __ballot(ok);
+            plain = __ballot(ok && tile * 16 + 15 <= see_first && (a.window == 0 || tile * 16 > see_last - a.window || tile * 16 + 15 < a.sinks));
+        };
+        auto load_step = [&](int k, Piece<D> (&x)[2]) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                int id = __builtin_amdgcn_readlane(ids, 2 * (k & 31) + u);
-                page[u] = id >= 0 && id < kv.n_pages ? id : -1;
-                id = page[u] < 0 ? 0 : id;
-                const uint8_t *tile = pool + id * kv.page_bytes + (tile_of(k, u) & tile_mask) * kv_tile_bytes(D);
-                load_piece<D>(tile, g, n, x[u]);
+                const int l = 2 * (k & 31) + u;
+                const uint32_t lo = __builtin_amdgcn_readlane((int)tile_at, l), hi = __builtin_amdgcn_readlane((int)(tile_at >> 32), l);
+                load_piece<D>(pool + ((uint64_t)hi << 32 | lo), g, n, x[u]);
             }
         };
+        // what the loads of a step need to be told of it: whether its tiles are there, and plain (two bits each)
+        auto flags_of = [&](int k) { return (uint32_t)(there >> (2 * (k & 31)) & 3u) | (uint32_t)(plain >> (2 * (k & 31)) & 3u) << 2; };
 
-        Piece<D> next[2];
-        int next_page[2];
-        if (steps > 0) load_step(0, next, next_page);
-        for (int k = 0; k < steps; ++k) {
-            Piece<D> x[2];
-            int page[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                x[u] = next[u];
-                page[u] = next_page[u];
-            }
-            if (((k + 1) & 31) == 0) ids = ids_of(k + 1);
-            if (k + 1 < steps) load_step(k + 1, next, next_page);
-
-            const int base0 = tile_of(k, 0) * 16, base1 = tile_of(k, 1) * 16;   // first tokens
-            const int hi_token = base1 + 15 > base0 + 15 ? base1 + 15 : base0 + 15;
-            const int lo_token = base0 < base1 ? base0 : base1;
-            const bool all_seen = page[0] >= 0 && page[1] >= 0 && hi_token <= see_first &&
-                                  (a.window == 0 || lo_token > see_last - a.window || hi_token < a.sinks);
-
-            // scores
+        auto step = [&](Piece<D> (&x)[2], uint32_t flags, int k) {
+            // scores, not scaled yet
             f32x4 s[NQ][2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 uint4 kf[KI];
 #pragma unroll
                 for (int j = 0; j < KI; ++j) {
-                    const float power = __uint_as_float((D == 256 && j >= KI / 2 ? x[u].k_power >> 8 : x[u].k_power & 255u) << 23);
+                    const float power = __uint_as_float((D == 256 ? (j >= KI / 2 ? x[u].k_power >> 8 : x[u].k_power & 255u) : x[u].k_power) << 23);
                     kf[j] = make_uint4(two<0>(x[u].k[j], power), two<1>(x[u].k[j], power), two<2>(x[u].k[j], power), two<3>(x[u].k[j], power));
                 }
 #pragma unroll
@@ -291,24 +278,19 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
                     s[t][u] = c;
                 }
             }
-#pragma unroll
-            for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[t][u][i] *= a.scale;
 
             uint64_t odd[2] = {0, 0};   // lanes of values that hold a block without a finite power
-            if (!all_seen) {
+            if (flags != 15u) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int j0 = (u ? base1 : base0) + 4 * g;
+                    const bool page = flags >> u & 1u;
+                    const int j0 = tile_of(k, u) * 16 + 4 * g;
 #pragma unroll
                     for (int t = 0; t < NQ; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int j = j0 + i;
-                            const bool sees = page[u] >= 0 && j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
+                            const bool sees = page && j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
                             s[t][u][i] = sees ? s[t][u][i] : MINUS_INF;
                         }
                     // values: powers of tokens behind the last one, and of blocks that are NaN, count as the smallest
@@ -317,12 +299,12 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t b = (x[u].v_power >> (8 * i)) & 255u;
-                        const bool there = page[u] >= 0 && j0 + i <= see_last;
-                        keep |= there && b < 254u ? b << (8 * i) : 0u;
-                        nan = nan || (there && b >= 254u);
+                        const bool in = page && j0 + i <= see_last;
+                        keep |= in && b < 254u ? b << (8 * i) : 0u;
+                        nan = nan || (in && b >= 254u);
                     }
                     odd[u] = __ballot(nan);
-                    if (odd[u] == 0 || !nan) x[u].v_power = keep;
+                    if (!nan) x[u].v_power = keep;
                 }
             }
 
@@ -332,10 +314,10 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             for (int t = 0; t < NQ; ++t) {
                 float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
                                   fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-                if (__any(top > m[t] + 8.0f)) {
+                if (__any(top * a.scale > m[t] + 8.0f)) {
                     top = fmaxf(top, __shfl_xor(top, 16, 64));
                     top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float grown = fmaxf(m[t], top);
+                    const float grown = fmaxf(m[t], top * a.scale);
                     const float shrink = m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(m[t] - grown);
                     m[t] = grown;
                     l[t] *= shrink;
@@ -346,8 +328,8 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
                 float p[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(s[t][0][i] - ref);
-                    p[4 + i] = __builtin_amdgcn_exp2f(s[t][1][i] - ref);
+                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][0][i], a.scale, -ref));
+                    p[4 + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][1][i], a.scale, -ref));
                 }
                 l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
                 uint32_t hi[4];
@@ -371,11 +353,11 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
                     for (int quad = 0; quad < 4; ++quad)
 #pragma unroll 1
                         for (int i = 0; i < 4; ++i) {
-                            const int j = (u ? base1 : base0) + 4 * quad + i;
+                            const int j = tile_of(k, u) * 16 + 4 * quad + i;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const uint32_t w = (uint32_t)__shfl((int)x[u].v_power, quad * 16 + 4 * g + e, 64);
-                                const bool bad = page[u] >= 0 && j <= see_last && ((w >> (8 * i)) & 255u) >= 254u;
+                                const bool bad = (flags >> u & 1u) && j <= see_last && ((w >> (8 * i)) & 255u) >= 254u;
 #pragma unroll
                                 for (int t = 0; t < NQ; ++t) {
                                     const bool sees = bad && j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
@@ -396,16 +378,20 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             }
 
             // outputs: token i of the lane's eight is token i % 4 of tile i / 4
+            float power[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int sh = 8 * (i & 3);
+                const uint32_t vp = x[i >> 2].v_power;
+                power[i] = __uint_as_float(sh == 24 ? vp >> 1 & 0x7f800000u : vp << (23 - sh) & 0x7f800000u);
+            }
 #pragma unroll
             for (int c = 0; c < NI / 2; ++c) {   // codes 2 c, 2 c + 1 of the lane's sixteenth
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int byte = (i & 3) * (D / 32) + c;
-                    const int sh = 8 * (i & 3);
-                    const uint32_t vp = x[i >> 2].v_power;
-                    const float power = __uint_as_float(sh == 24 ? vp >> 1 & 0x7f800000u : vp << (23 - sh) & 0x7f800000u);
-                    w[i] = two_at(x[i >> 2].v[byte >> 2], power, byte & 3);
+                    w[i] = two_at(x[i >> 2].v[byte >> 2], power[i], byte & 3);
                 }
                 uint4 even, second;
                 even = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
@@ -422,6 +408,21 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
                     }
                 }
             }
+        };
+
+        // two steps a turn, the loads of the next one under way during each: no register is moved
+        Piece<D> xa[2], xb[2];
+        if (steps > 0) {
+            look_up(0);
+            load_step(0, xa);
+        }
+        for (int k = 0; k < steps; k += 2) {
+            const uint32_t fa = flags_of(k), fb = flags_of(k + 1);
+            if (k + 1 < steps) load_step(k + 1, xb);
+            step(xa, fa, k);
+            if (((k + 2) & 31) == 0 && k + 2 < steps) look_up(k + 2);
+            if (k + 2 < steps) load_step(k + 2, xa);
+            if (k + 1 < steps) step(xb, fb, k + 1);
         }
 
         // sums over the four lanes of a row
@@ -525,48 +526,58 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
     }
 }
 
-// joins the parts of rows that were split: 16 threads per row
+// Joins the parts of rows that were split, a wave per row: lane p has part p's maximum and factor, and the sums are read D / 64 numbers a lane, eight
+// parts under way at once.  Bound by those trips to memory: few rows have many parts.
+constexpr int MAX_PARTS = 64;
 template <int D, bool HALF>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, int group_rows)
+__global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, int group_rows, int slices)
 {
-    const Place at = place_of(kv, a, 1);
-    if (at.r < 0) return;
-    const Request rq = request_of(kv, a, at.r);
+    const int lane = threadIdx.x & 63;
+    const int slice = blockIdx.x % slices;                         // of the row tile's rows
+    const uint32_t unit = blockIdx.x / slices;
+    const int rt0 = (int)(unit % a.row_tiles), pair = (int)(unit / a.row_tiles);
+    const int r = pair / kv.n_heads, h = pair % kv.n_heads;
+    const Request rq = request_of(kv, a, r);
     const int rows = rq.count * a.group, heads = kv.n_heads * a.group;
     const int64_t all_rows = a.Qt * heads;
-    for (int rt = at.rt; rt * group_rows < rows; rt += a.row_tiles) {
+    for (int rt = rt0; rt * group_rows < rows; rt += a.row_tiles) {
         const int row_a = rt * group_rows, row_b = (rows < row_a + group_rows ? rows : row_a + group_rows) - 1;
-        const int p0 = rq.len - rq.count;
-        const Span sp = span_of(a, p0 + row_a / a.group, p0 + row_b / a.group);
+        const int q0 = rq.len - rq.count;
+        const Span sp = span_of(a, q0 + row_a / a.group, q0 + row_b / a.group);
         if (sp.parts == 1) continue;
-        for (int row = row_a + (threadIdx.x >> 4); row <= row_b; row += 16) {
-            const int i16 = threadIdx.x & 15;
-            const int i = row / a.group, head = at.h * a.group + row - i * a.group;
+        for (int row = row_a + slice * 4 + (int)(threadIdx.x >> 6); row <= row_b; row += slices * 4) {
+            const int i = row / a.group, head = h * a.group + row - i * a.group;
             const int64_t x = (rq.first + i) * heads + head;
-            float m = MINUS_INF, l = 0.0f;
-            for (int p = 0; p < sp.parts; ++p) m = fmaxf(m, a.part_stat[(p * all_rows + x) * 2]);
-            float y[D / 16] = {};
-            for (int p = 0; p < sp.parts; ++p) {
-                const float mp = a.part_stat[(p * all_rows + x) * 2];
-                if (mp == MINUS_INF) continue;   // a part of which the row sees nothing
-                const float f = __builtin_amdgcn_exp2f(mp - m);
-                l += f * a.part_stat[(p * all_rows + x) * 2 + 1];
+            const float2 stat = lane < sp.parts ? *reinterpret_cast<const float2 *>(a.part_stat + (lane * all_rows + x) * 2) : make_float2(MINUS_INF, 0.0f);
+            float m = stat.x;
 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) {
-                    const float4 v = *reinterpret_cast<const float4 *>(a.part_out + (p * all_rows + x) * D + c * 64 + i16 * 4);
-                    y[4 * c] += f * v.x, y[4 * c + 1] += f * v.y, y[4 * c + 2] += f * v.z, y[4 * c + 3] += f * v.w;
+            for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+            const float f = stat.x == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(stat.x - m);   // 0: a part of which the row sees nothing
+            float l = f * stat.y;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) l += __shfl_xor(l, s, 64);
+            float y[D / 64] = {};
+            const float *src = a.part_out + x * D + lane * (D / 64);
+            for (int p0 = 0; p0 < sp.parts; p0 += 8) {
+                float v[8][D / 64];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int64_t p = p0 + e < sp.parts ? p0 + e : sp.parts - 1;
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) v[e][c] = src[p * all_rows * D + c];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (p0 + e) & 63));   // 0 behind the last part
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) y[c] += fp == 0.0f || p0 + e >= sp.parts ? 0.0f : fp * v[e][c];   // what a part of factor 0 holds may be anything
                 }
             }
-            const float f = l == 0.0f ? 0.0f : 1.0f / l;
+            const float over = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t *dst = static_cast<uint16_t *>(a.out) + (rq.first + i) * a.out_token + head * a.out_head + lane * (D / 64);
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                const float z0 = y[4 * c] * f, z1 = y[4 * c + 1] * f, z2 = y[4 * c + 2] * f, z3 = y[4 * c + 3] * f;
-                uint2 z;
-                if constexpr (HALF) z = make_uint2(f32_to_f16_bits(z0) | f32_to_f16_bits(z1) << 16, f32_to_f16_bits(z2) | f32_to_f16_bits(z3) << 16);
-                else z = make_uint2(pack_bf16(z0, z1), pack_bf16(z2, z3));
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + (rq.first + i) * a.out_token + head * a.out_head + c * 64 + i16 * 4) = z;
-            }
-            if (i16 == 0 && a.lse) a.lse[x] = l == 0.0f ? MINUS_INF : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+            for (int c = 0; c < D / 64; ++c) dst[c] = HALF ? f32_to_f16_bits(y[c] * over) : pack_bf16(y[c] * over, 0.0f);
+            if (lane == 0 && a.lse) a.lse[x] = l == 0.0f ? MINUS_INF : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
         }
     }
 }
@@ -584,7 +595,11 @@ hipError_t run(const KvView &kv, const KvAttention &a, const KvAttentionPlan &pl
         if (e != hipSuccess) return e;
     }
     kv_attention_kernel<D, NQ, HALF, ROWS><<<(unsigned)(groups * plan.parts), 256, lds, stream>>>(kv, a);
-    if (plan.parts > 1) kv_join_kernel<D, HALF><<<(unsigned)groups, 256, 0, stream>>>(kv, a, plan.rows);
+    if (plan.parts > 1) {
+        // four rows of a row tile per workgroup, if there are that many
+        const int most = (int)ceil_div(plan.rows < a.max_rows ? plan.rows : a.max_rows, 4);
+        kv_join_kernel<D, HALF><<<(unsigned)((int64_t)kv.R * kv.n_heads * plan.row_tiles * most), 256, 0, stream>>>(kv, a, plan.rows, most);
+    }
     return hipGetLastError();
 }
 template <int D, bool HALF>
@@ -606,6 +621,7 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     p.form = rows <= 16 ? KV_FORM_TOKENS16 : rows <= 32 && d < 256 ? KV_FORM_TOKENS32 : KV_FORM_ROWS;   // 32 rows of 256 numbers do not fit the registers
     p.rows = p.form == KV_FORM_TOKENS16 ? 16 : p.form == KV_FORM_TOKENS32 ? 32 : d == 256 ? 64 : 128;
     p.row_tiles = (int32_t)ceil_div(rows, p.rows);
+    p.max_rows = (int32_t)(rows < 0x7fffffff ? rows : 0x7fffffff);
     // tokens that a row tile may see
     int64_t seen = max_len < 1 ? 1 : max_len;
     if (window > 0) {
@@ -614,11 +630,11 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     }
     const int64_t tiles = ceil_div(seen, KV_TILE);
     const int64_t groups = R * n_heads * p.row_tiles;
-    // workgroups for eight rounds of the chip's 256 CUs, if the parts do not get shorter than two steps of each wave
+    // three workgroups for each of the 256 CUs, which is what their registers allow, if the parts do not get shorter than two steps of each wave
     const int64_t least = p.form == KV_FORM_ROWS ? 8 : 16;
-    int64_t parts = ceil_div(2048, groups);
+    int64_t parts = ceil_div(768, groups);
     if (parts > ceil_div(tiles, least)) parts = ceil_div(tiles, least);
-    if (parts > 64) parts = 64;
+    if (parts > MAX_PARTS) parts = MAX_PARTS;
     p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);
     return p;
