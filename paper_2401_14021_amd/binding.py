@@ -145,7 +145,13 @@ def _check(status: int) -> None:
         raise RalmError(status, lib().ralm_last_error().decode())
 
 
+# the current stream's handle without a Stream object around it (2.8 us a call on the host, 0.3 so)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 

@@ -8,11 +8,11 @@
 // the floor are exact in fp32, differences and sums in 64 bits, so no order of summation can show and a token is the same however a row is
 // split: the smallest one whose running sum exceeds floor(m S / 2^24), S the sum of all.
 //
-//  draft_sums_kernel   a wave per 1024 entries of a request's row: accepts (again in every wave: 3 loads in a row, no launch of their
-//                      own) and the sums of the entries
+//  draft_sums_kernel   a wave per 1024 entries of a request's row, or some of them where there are many: accepts (again in every wave: 3
+//                      loads in a row, no launch of their own) and the sums of the entries
 //  draft_pick_kernel   a workgroup per request: the 1024 entries in which the running sum passes the line, and the entry
-// Rows are read once, but for the 1024 entries that hold the token; what bounds a small call is the chain offsets -> drafts ->
-// probabilities -> row.
+// Rows are read once, but for the 1024 entries that hold the token.  What bounds a small call is the chain offsets -> drafts ->
+// probabilities -> row, a large one the conversion of the entries (two to doubles, a difference, a maximum and a sum of doubles each).
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "kv_kernels.h"
@@ -34,22 +34,22 @@ __device__ __forceinline__ float entry(const void *p, int64_t i)
 __device__ __forceinline__ float fixed(float p) { return floorf(fminf(fmaxf(p, 0.0f), 1.0f) * FIX); }
 __device__ __forceinline__ u64 random24(float u) { return (u64)(fminf(fmaxf(u, 0.0f), 0.99999994f) * 16777216.0f); }
 
-// four entries of a row from i on (4-byte aligned for fp32, 2-byte for the others), zeros behind V
-template <int DT>
-__device__ __forceinline__ void entries4(const void *row, int64_t i, int V, float (&x)[4])
+// N entries of a row from i on, which is aligned to its type alone: one load of up to 16 bytes; zeros behind V
+template <int DT, int N>
+__device__ __forceinline__ void entries(const void *row, int64_t i, int V, float (&x)[N])
 {
-    if (i + 4 <= V) {
+    if (i + N <= V) {
         if constexpr (DT == DT_F32) {
-            __builtin_memcpy(x, static_cast<const float *>(row) + i, 16);
+            __builtin_memcpy(x, static_cast<const float *>(row) + i, 4 * N);
         } else {
-            uint16_t h[4];
-            __builtin_memcpy(h, static_cast<const uint16_t *>(row) + i, 8);
+            uint16_t h[N];
+            __builtin_memcpy(h, static_cast<const uint16_t *>(row) + i, 2 * N);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = DT == DT_F16 ? f16_bits_to_f32(h[j]) : __uint_as_float((uint32_t)h[j] << 16);
+            for (int j = 0; j < N; ++j) x[j] = DT == DT_F16 ? f16_bits_to_f32(h[j]) : __uint_as_float((uint32_t)h[j] << 16);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = i + j < V ? entry<DT>(row, i + j) : 0.0f;
+        for (int j = 0; j < N; ++j) x[j] = i + j < V ? entry<DT>(row, i + j) : 0.0f;
     }
 }
 
@@ -91,47 +91,51 @@ __device__ __forceinline__ Rows rows_of(const DraftParams &p, int64_t r, int64_t
     w.hot = n < count && !p.draft_probs ? p.draft_ids[first + n] : -1;
     return w;
 }
-// four entries' weights: what is left of the target, and the target alone (whole numbers)
-template <int DT>
-__device__ __forceinline__ void weights4(const Rows &w, int64_t i, int V, double (&left)[4], double (&all)[4])
+// N entries' weights (whole numbers)
+template <int DT, int N>
+__device__ __forceinline__ void weights(const Rows &w, int64_t i, int V, double (&x)[N])
 {
-    float p[4], q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    entries4<DT>(w.p, i, V, p);
-    if (w.q) entries4<DT>(w.q, i, V, q);
+    float p[N], q[N] = {};
+    entries<DT, N>(w.p, i, V, p);
+    if (w.q) entries<DT, N>(w.q, i, V, q);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        all[j] = fixed(p[j]);
-        left[j] = i + j == w.hot ? 0.0 : fmax(all[j] - (double)fixed(q[j]), 0.0);
+    for (int j = 0; j < N; ++j) x[j] = i + j == w.hot ? 0.0 : fmax((double)fixed(p[j]) - (double)fixed(q[j]), 0.0);
+}
+// the sum of chunk c's weights, by all lanes of a wave; 1024 entries of at most 2^36 are exact in a double
+template <int DT>
+__device__ __forceinline__ u64 chunk_sum(const Rows &w, int64_t c, int V)
+{
+    constexpr int N = DT == DT_F32 ? 4 : 8;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < DRAFT_CHUNK / (64 * N); ++i) {
+        double x[N];
+        weights<DT, N>(w, c * DRAFT_CHUNK + i * (64 * N) + (threadIdx.x & 63) * N, V, x);
+#pragma unroll
+        for (int j = 0; j < N; j += 4) sum += (x[j] + x[j + 1]) + (x[j + 2] + x[j + 3]);
     }
+    return (u64)wave64_sum(sum);
 }
 __device__ __forceinline__ int64_t clamp_row(int64_t o, int64_t n) { return o < 0 ? 0 : o > n ? n : o; }
 
+// per: chunks of a wave
 template <int DT>
-__global__ __launch_bounds__(256) void draft_sums_kernel(DraftParams p)
+__global__ __launch_bounds__(256) void draft_sums_kernel(DraftParams p, int per)
 {
     const int lane = threadIdx.x & 63;
+    const int64_t waves = (p.chunks + per - 1) / per;   // of a request
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= p.R * p.chunks) return;
-    const int64_t r = unit / p.chunks, c = unit % p.chunks;
+    if (unit >= p.R * waves) return;
+    const int64_t r = unit / waves, c0 = unit % waves * per, c1 = c0 + per < p.chunks ? c0 + per : p.chunks;
     const int64_t first = clamp_row(p.offsets[r], p.Qt), end = clamp_row(p.offsets[r + 1], p.Qt);
     const int count = end > first ? (int)(end - first) : 0;
     const int n = accepted_of<DT>(p, r, first, count);
-    if (c == 0 && lane == 0) p.accepted[r] = n;
+    if (c0 == 0 && lane == 0) p.accepted[r] = n;
     const Rows w = rows_of<DT>(p, r, first, count, n);
-    double left = 0.0, all = 0.0;   // 16 entries of at most 2^36: exact
-#pragma unroll
-    for (int i = 0; i < DRAFT_CHUNK / 256; ++i) {
-        double a[4], b[4];
-        weights4<DT>(w, c * DRAFT_CHUNK + i * 256 + lane * 4, p.V, a, b);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            left += a[j];
-            all += b[j];
-        }
+    for (int64_t c = c0; c < c1; ++c) {
+        const u64 sum = chunk_sum<DT>(w, c, p.V);
+        if (lane == 0) p.sums[r * p.chunks + c] = sum;
     }
-    left = wave64_sum(left);   // up to 2^46
-    all = wave64_sum(all);
-    if (lane < 2) p.sums[unit * 2 + lane] = (u64)(lane ? all : left);
 }
 
 __device__ __forceinline__ u64 shfl_up_u64(u64 v, int s)
@@ -169,28 +173,36 @@ __global__ __launch_bounds__(256) void draft_pick_kernel(DraftParams p)
     const int tid = threadIdx.x;
     const int64_t first = clamp_row(p.offsets[r], p.Qt), end = clamp_row(p.offsets[r + 1], p.Qt);
     const int count = end > first ? (int)(end - first) : 0;
-    const u64 *sums = p.sums + r * p.chunks * 2;
+    u64 *sums = p.sums + r * p.chunks;
+    const u64 m = random24(p.u_next[r]);
+    Rows w = rows_of<DT>(p, r, first, count, p.accepted[r]);
     // neighbouring chunks per thread
     const int64_t per = (p.chunks + 255) / 256, c0 = tid * per, c1 = c0 + per < p.chunks ? c0 + per : p.chunks;
-    u64 mine[2] = {0, 0}, total[2];
-    for (int64_t c = c0; c < c1; ++c) {
-        mine[0] += sums[2 * c];
-        mine[1] += sums[2 * c + 1];
+    u64 mine, before, S;
+    for (int again = 0;; ++again) {
+        mine = 0;
+        for (int64_t c = c0; c < c1; ++c) mine += sums[c];
+        before = sum_before(mine, red, S);
+        if (S != 0 || again || (!w.q && w.hot < 0)) break;
+        // nothing is left beside the draft: the target alone
+        w.q = nullptr;
+        w.hot = -1;
+        for (int64_t c = tid >> 6; c < p.chunks; c += 4) {
+            const u64 sum = chunk_sum<DT>(w, c, p.V);
+            if ((tid & 63) == 0) sums[c] = sum;
+        }
+        __threadfence_block();
+        __syncthreads();
     }
-    u64 before0 = sum_before(mine[0], red, total[0]);
-    const u64 before1 = sum_before(mine[1], red, total[1]);
-    const int kind = total[0] == 0;   // nothing is left beside the draft: the target alone
-    const u64 S = total[kind];
     if (S == 0) {
         if (tid == 0) p.next[r] = -1;
         return;
     }
-    const u64 m = random24(p.u_next[r]);
     const u64 t = __umul64hi(m, S) << 40 | (m * S) >> 24;   // < S
-    u64 run = kind ? before1 : before0;
-    if (t >= run && t - run < mine[kind]) {   // one thread alone
+    u64 run = before;
+    if (t >= run && t - run < mine) {   // one thread alone
         for (int64_t c = c0; c < c1; ++c) {
-            const u64 x = sums[2 * c + kind];
+            const u64 x = sums[c];
             if (t - run < x) {
                 s_chunk = c;
                 s_before = run;
@@ -201,15 +213,11 @@ __global__ __launch_bounds__(256) void draft_pick_kernel(DraftParams p)
     }
     __syncthreads();
     const int64_t i = s_chunk * DRAFT_CHUNK + tid * 4;
-    const Rows w = rows_of<DT>(p, r, first, count, p.accepted[r]);
-    double left[4], all[4];
-    weights4<DT>(w, i, p.V, left, all);
+    double y[4];
+    weights<DT, 4>(w, i, p.V, y);
     u64 x[4], sum = 0, whole;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        x[j] = (u64)(kind ? all[j] : left[j]);
-        sum += x[j];
-    }
+    for (int j = 0; j < 4; ++j) sum += x[j] = (u64)y[j];
     run = s_before + sum_before(sum, red, whole);
     if (t >= run && t - run < sum) {
         int j = 0;
@@ -221,7 +229,9 @@ __global__ __launch_bounds__(256) void draft_pick_kernel(DraftParams p)
 template <int DT>
 hipError_t verify_draft(const DraftParams &p, hipStream_t stream)
 {
-    draft_sums_kernel<DT><<<(unsigned)((p.R * p.chunks + 3) / 4), 256, 0, stream>>>(p);
+    // a wave of its own per chunk while all waves are on the chip at once (256 CUs, 16 waves each)
+    const int per = (int)((p.R * p.chunks + 4095) / 4096), waves = (int)((p.chunks + per - 1) / per);
+    draft_sums_kernel<DT><<<(unsigned)((p.R * waves + 3) / 4), 256, 0, stream>>>(p, per);
     draft_pick_kernel<DT><<<(unsigned)p.R, 256, 0, stream>>>(p);
     return hipGetLastError();
 }

@@ -272,7 +272,7 @@ ralm_status ralm_kv_compact(const ralm_kv_t *kv, int32_t *table_out, int32_t *re
 size_t ralm_verify_draft_workspace_bytes(int64_t R, int32_t V)
 {
     if (R < 1 || R > MAX_KV_REQUESTS || V < 1 || V > RALM_MAX_VOCABULARY) return 0;
-    return (size_t)R * draft_chunks(V) * 16;
+    return (size_t)R * draft_chunks(V) * 8;
 }
 
 ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs, int64_t draft_stride, const void *target_probs, int64_t target_stride,

@@ -98,7 +98,7 @@ struct DraftParams {
     const int64_t *offsets;
     int64_t Qt, R;
     int32_t *accepted, *next;
-    unsigned long long *sums;   // [R][chunks][2]: what is left of the target beside the draft, and the target alone
+    unsigned long long *sums;   // [R][chunks]
     int64_t chunks;
 };
 constexpr int DRAFT_CHUNK = 1024;   // entries of a row that a wave sums up
