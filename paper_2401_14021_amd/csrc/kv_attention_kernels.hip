@@ -75,12 +75,16 @@ __device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[W])
     }
 }
 template <int D>
-__device__ __forceinline__ void load_piece(const uint8_t *tile, int g, int n, Piece<D> &x)
+__device__ __forceinline__ void load_keys(const uint8_t *tile, int g, int n, Piece<D> &x)
 {
     load_words<D / 32>(tile + n * (D / 2) + g * (D / 8), x.k);
-    load_words<D / 32>(tile + 8 * D + g * (2 * D) + n * (D / 8), x.v);
     const uint8_t *kp = tile + 16 * D + n * (D / 32);
     x.k_power = D == 64 ? kp[g >> 1] : D == 128 ? kp[g] : *reinterpret_cast<const uint16_t *>(kp + 2 * g);
+}
+template <int D>
+__device__ __forceinline__ void load_values(const uint8_t *tile, int g, int n, Piece<D> &x)
+{
+    load_words<D / 32>(tile + 8 * D + g * (2 * D) + n * (D / 8), x.v);
     x.v_power = *reinterpret_cast<const uint32_t *>(tile + 16 * D + D / 2 + g * (D / 8) + n * D / 512 * 4);
 }
 
@@ -100,10 +104,13 @@ __device__ __forceinline__ Span span_of(const KvAttention &a, int p_first, int p
     const int n = s.sinks + tiles_up_to(p_last) - s.lo;
     s.n = n < 0 || p_last < 0 ? 0 : n;
     const int per = (s.n + a.parts - 1) / a.parts;
-    s.part = a.part_tiles > per ? a.part_tiles : (per + 1) / 2 * 2;
+    s.part = a.part_tiles > per ? a.part_tiles : (per + 3) / 4 * 4;
     s.parts = s.n == 0 ? 1 : (s.n + s.part - 1) / s.part;
     return s;
 }
+
+// the v-th tile of a span's list
+__device__ __forceinline__ int listed_tile(const Span &s, int v) { return v < s.sinks ? v : v - s.sinks + s.lo; }
 
 struct Request {
     int64_t first;    // row of q and out
@@ -141,18 +148,223 @@ __device__ __forceinline__ Place place_of(const KvView &kv, const KvAttention &a
     return x;
 }
 
-template <int D>
-constexpr int lds_bytes(int nq, bool rows) { return rows ? 16 : 4 * 16 * (D + 4) * 4 + 2 * 4 * 16 * nq * 4; }
+// NQ * 16 rows of a key/value head that a wave works on
+template <int D, int NQ, bool HALF>
+struct Block {
+    static constexpr int KI = D / 32, NI = D / 16;   // multiplies per tile: scores, outputs
+    int pos[NQ];             // place of the row's query; -1: no row
+    uint4 qf[NQ][KI], ql[HALF ? NQ : 1][HALF ? KI : 1];
+    f32x4 o[NQ][NI];
+    float m[NQ], l[NQ];
+    int see_first, see_last;   // places of the first and last row's query; -1: no rows
 
-// ROWS: each of the four waves has NQ * 16 rows of its own and goes over all tokens of the part (many rows); else all waves have the same
-// NQ * 16 rows and share out the part's tokens, 32 at a time (few rows).
+    // rows row_a .. row_b (at most) of request rq
+    __device__ __forceinline__ void begin(const KvAttention &a, const Request &rq, int h, int row_a, int row_b)
+    {
+        const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+        const int p0 = rq.len - rq.count;
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            const int row = row_a + t * 16 + n;
+            const bool real = row <= row_b;
+            const int i = real ? row / a.group : 0, head = h * a.group + (real ? row - i * a.group : 0);
+            pos[t] = real ? p0 + i : -1;
+            const uint16_t *q = static_cast<const uint16_t *>(a.q) + (rq.first + i) * a.q_token + head * a.q_head + g * (D / 4);
+#pragma unroll
+            for (int j = 0; j < KI; ++j) {
+                uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                if (real) x = *reinterpret_cast<const uint4 *>(q + 8 * j);
+                if constexpr (HALF) {
+                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float f0 = f16_bits_to_f32(u[c] & 0xffffu), f1 = f16_bits_to_f32(u[c] >> 16);
+                        hi[c] = pack_bf16(f0, f1);
+                        lo[c] = pack_bf16(f0 - low(hi[c]), f1 - high(hi[c]));
+                    }
+                    x = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    y = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+                qf[t][j] = x;
+                if constexpr (HALF) ql[t][j] = y;
+            }
+            m[t] = MINUS_INF;
+            l[t] = 0.0f;
+#pragma unroll
+            for (int i2 = 0; i2 < NI; ++i2) o[t][i2] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        const int last = row_b < row_a + NQ * 16 - 1 ? row_b : row_a + NQ * 16 - 1;
+        see_first = row_a <= row_b ? p0 + row_a / a.group : 0;
+        see_last = row_a <= row_b ? p0 + last / a.group : -1;
+    }
+    __device__ __forceinline__ bool sees(const KvAttention &a, int t, int j) const
+    {
+        return j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
+    }
+    // whether all rows see all of a tile
+    __device__ __forceinline__ bool all_see(const KvAttention &a, int tile) const
+    {
+        return tile * 16 + 15 <= see_first && (a.window == 0 || tile * 16 > see_last - a.window || tile * 16 + 15 < a.sinks);
+    }
+    __device__ __forceinline__ void mask(const KvAttention &a, f32x4 (&s)[2], int t, int u, bool page, int j0) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[u][i] = page && sees(a, t, j0 + i) ? s[u][i] : MINUS_INF;
+    }
+    // running maximum, p, sum: the weights of the lane's eight tokens for its row of block t
+    __device__ __forceinline__ void weigh(const KvAttention &a, int t, const f32x4 (&s)[2], uint4 &pf, uint4 &pl)
+    {
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        if (__any(top * a.scale > m[t] + 8.0f)) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float grown = fmaxf(m[t], top * a.scale);
+            const float shrink = m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(m[t] - grown);
+            m[t] = grown;
+            l[t] *= shrink;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) o[t][i] *= shrink;
+        }
+        const float ref = m[t] == MINUS_INF ? 0.0f : m[t];
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i], a.scale, -ref));
+            p[4 + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][i], a.scale, -ref));
+        }
+        l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        uint32_t hi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hi[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+        pf = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if constexpr (HALF) {
+            uint32_t lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lo[i] = pack_bf16(p[2 * i] - low(hi[i]), p[2 * i + 1] - high(hi[i]));
+            pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+    }
+    // Values of a tile (first token j0, powers v_power by lane) whose power is not finite: NaN for the rows that see them and no others.  A lane of O^T
+    // holds the sixteenths 4 g .. 4 g + 3 of row n, the power of which lies with lane (quad, sixteenth)
+    __device__ __forceinline__ void spoil(const KvAttention &a, uint32_t v_power, bool page, int j0)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll 1
+        for (int quad = 0; quad < 4; ++quad)
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t w = (uint32_t)__shfl((int)v_power, quad * 16 + 4 * g + e, 64);
+                    const bool bad = page && ((w >> (8 * i)) & 255u) >= 254u;
+#pragma unroll
+                    for (int t = 0; t < NQ; ++t)
+#pragma unroll
+                        for (int c = 0; c < NI; ++c)
+                            if (bad && sees(a, t, j0 + 4 * quad + i)) o[t][c][e] = __builtin_nanf("");
+                }
+    }
+    // sums over the four lanes of a row
+    __device__ __forceinline__ void end()
+    {
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            l[t] += __shfl_xor(l[t], 16, 64);
+            l[t] += __shfl_xor(l[t], 32, 64);
+        }
+    }
+};
+
+// what values' powers count as: those of tokens behind j_last, and those that are not finite, as the smallest.  bad: whether there were any of
+// the latter
+__device__ __forceinline__ uint32_t guard_values(uint32_t v_power, bool page, int j0, int j_last, bool &bad)
+{
+    uint32_t keep = 0;
+    bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b = (v_power >> (8 * i)) & 255u;
+        const bool in = page && j0 + i <= j_last;
+        keep |= in && b < 254u ? b << (8 * i) : 0u;
+        bad = bad || (in && b >= 254u);
+    }
+    return keep;
+}
+// the four powers of a word as fp32
+__device__ __forceinline__ void powers(uint32_t v_power, float *p)
+{
+    p[0] = __uint_as_float(v_power << 23);
+    p[1] = __uint_as_float(v_power << 15 & 0x7f800000u);
+    p[2] = __uint_as_float(v_power << 7 & 0x7f800000u);
+    p[3] = __uint_as_float(v_power >> 1 & 0x7f800000u);
+}
+template <int D>
+__device__ __forceinline__ float k_power_of(uint32_t k_power, int j)
+{
+    return __uint_as_float((D == 256 ? (j >= D / 64 ? k_power >> 8 : k_power & 255u) : k_power) << 23);
+}
+// operand of the j-th multiply of a tile's scores
+__device__ __forceinline__ uint4 k_operand(uint32_t codes, float power) { return make_uint4(two<0>(codes, power), two<1>(codes, power), two<2>(codes, power), two<3>(codes, power)); }
+// operands of the multiplies for codes 2 c and 2 c + 1 of the lane's sixteenth: token i of the lane's eight is token i % 4 of tile i / 4
+template <int D>
+__device__ __forceinline__ void v_operands(const uint32_t (&va)[D / 32], const uint32_t (&vb)[D / 32], const float (&power)[8], int c, uint4 &even, uint4 &odd)
+{
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int byte = (i & 3) * (D / 32) + c;
+        w[i] = two_at(i < 4 ? va[byte >> 2] : vb[byte >> 2], power[i], byte & 3);
+    }
+    even = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
+                      __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u));
+    odd = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u),
+                     __builtin_amdgcn_perm(w[5], w[4], 0x07060302u), __builtin_amdgcn_perm(w[7], w[6], 0x07060302u));
+}
+
+// results of a row: to the output where nothing was split, else to the part's place
+template <int D, bool HALF>
+struct Sink {
+    const KvAttention &a;
+    int heads, part;
+    bool whole;
+    int64_t all_rows;
+    __device__ __forceinline__ Sink(const KvView &kv, const KvAttention &a_, int part_, bool whole_)
+        : a(a_), heads(kv.n_heads * a_.group), part(part_), whole(whole_), all_rows(a_.Qt * kv.n_heads * a_.group) {}
+    // numbers d .. d + 3 of a row
+    __device__ __forceinline__ void put4(int64_t row, int head, int d, float y0, float y1, float y2, float y3) const
+    {
+        if (whole) {
+            uint2 z;
+            if constexpr (HALF) z = make_uint2(f32_to_f16_bits(y0) | f32_to_f16_bits(y1) << 16, f32_to_f16_bits(y2) | f32_to_f16_bits(y3) << 16);
+            else z = make_uint2(pack_bf16(y0, y1), pack_bf16(y2, y3));
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.out_token + head * a.out_head + d) = z;
+        } else {
+            *reinterpret_cast<float4 *>(a.part_out + (part * all_rows + row * heads + head) * D + d) = make_float4(y0, y1, y2, y3);
+        }
+    }
+    __device__ __forceinline__ void put_stat(int64_t row, int head, float m, float l) const
+    {
+        const int64_t i = row * heads + head;
+        if (whole) {
+            if (a.lse) a.lse[i] = l == 0.0f ? MINUS_INF : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+        } else {
+            *reinterpret_cast<float2 *>(a.part_stat + (part * all_rows + i) * 2) = make_float2(m, l);
+        }
+    }
+};
+
+// ROWS: each of a workgroup's four waves has NQ * 16 rows of its own and goes over all tokens of the part (many rows; the waves never wait for each
+// other).  Else all have the same NQ * 16 rows and share out the part's tokens, 32 at a time, and their sums meet in LDS (few rows).
+template <int D, int NQ, bool ROWS>
+constexpr int lds_bytes() { return ROWS ? 16 : 4 * 16 * (D + 4) * 4 + 2 * 4 * 16 * NQ * 4; }
+
 template <int D, int NQ, bool HALF, bool ROWS>
 __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttention a)
 {
-    constexpr int KI = D / 32, NI = D / 16;   // multiplies per tile: scores, outputs
-    constexpr int RW = NQ * 16;               // rows of a wave
-    constexpr int RG = ROWS ? 4 * RW : RW;    // of the workgroup
-    constexpr int STRIDE = ROWS ? 1 : 4;      // steps of a wave: every STRIDE-th
+    using B = Block<D, NQ, HALF>;
+    constexpr int KI = B::KI, NI = B::NI, RW = NQ * 16, RG = ROWS ? 4 * RW : RW;   // rows of a wave, of the workgroup
+    constexpr int STRIDE = ROWS ? 1 : 4;                                              // a wave's steps are every STRIDE-th
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
@@ -165,246 +377,104 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
     const int32_t *table = kv.table + (int64_t)at.r * kv.max_pages;
 
     for (int rt = at.rt; rt * RG < rows; rt += a.row_tiles) {
-        const int row_a = rt * RG, row_b = (rows < row_a + RG ? rows : row_a + RG) - 1;   // the workgroup's first and last row
-        const int p0 = rq.len - rq.count;                                                // place of the first query
-        const Span sp = span_of(a, p0 + row_a / a.group, p0 + row_b / a.group);
+        const int row_a = rt * RG, row_b = (rows < row_a + RG ? rows : row_a + RG) - 1;
+        const int q0 = rq.len - rq.count;   // place of the first query
+        const Span sp = span_of(a, q0 + row_a / a.group, q0 + row_b / a.group);
         if (at.part >= sp.parts) continue;
+        B b;
+        b.begin(a, rq, at.h, ROWS ? row_a + wave * RW : row_a, row_b);
 
-        // this wave's rows
-        const int w_a = ROWS ? row_a + wave * RW : row_a;
-        const int w_b = row_b < w_a + RW - 1 ? row_b : w_a + RW - 1;
-        const bool any_rows = w_a <= row_b;
-        int pos[NQ];                // place of the row's query; -1: no row
-        int64_t q_row[NQ];
-        int q_head[NQ];
-        uint4 qf[NQ][KI], ql[HALF ? NQ : 1][HALF ? KI : 1];
-#pragma unroll
-        for (int t = 0; t < NQ; ++t) {
-            const int row = w_a + t * 16 + n;
-            const bool real = row <= row_b;
-            const int i = real ? row / a.group : 0;
-            q_head[t] = at.h * a.group + (real ? row - i * a.group : 0);
-            q_row[t] = rq.first + i;
-            pos[t] = real ? p0 + i : -1;
-            const uint16_t *q = static_cast<const uint16_t *>(a.q) + q_row[t] * a.q_token + q_head[t] * a.q_head + g * (D / 4);
-#pragma unroll
-            for (int j = 0; j < KI; ++j) {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (real) x = *reinterpret_cast<const uint4 *>(q + 8 * j);
-                if constexpr (HALF) {
-                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float f0 = f16_bits_to_f32(u[c] & 0xffffu), f1 = f16_bits_to_f32(u[c] >> 16);
-                        hi[c] = pack_bf16(f0, f1);
-                        lo[c] = pack_bf16(f0 - low(hi[c]), f1 - high(hi[c]));
-                    }
-                    qf[t][j] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    ql[t][j] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                } else {
-                    qf[t][j] = x;
-                }
-            }
-        }
-        const int see_first = any_rows ? p0 + w_a / a.group : 0, see_last = any_rows ? p0 + w_b / a.group : -1;   // places of the wave's rows
-
-        f32x4 o[NQ][NI];
-        float m[NQ], l[NQ];
-#pragma unroll
-        for (int t = 0; t < NQ; ++t) {
-            m[t] = MINUS_INF;
-            l[t] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) o[t][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-
-        // the wave's tiles: [v0, v1) of the span's list
-        const int v0 = at.part * sp.part;
-        int v1 = v0 + sp.part < sp.n ? v0 + sp.part : sp.n;
-        const int own = sp.sinks + tiles_up_to(see_last) - sp.lo;   // tiles that the wave's last row sees
-        v1 = own < v1 ? own : v1;
-        const int steps = v1 > v0 ? ((v1 - v0 + 1) / 2 + STRIDE - 1 - (ROWS ? 0 : wave)) / STRIDE : 0;
+        // this wave's tiles: of the part's, [v0, v1) of the span's list, those that its last row sees; its steps are pairs of them
+        const int own = sp.sinks + tiles_up_to(b.see_last) - sp.lo;
+        const int v0 = at.part * sp.part, end = v0 + sp.part < sp.n ? v0 + sp.part : sp.n, v1 = own < end ? own : end;
         const int step0 = ROWS ? 0 : wave;
+        const int steps = v1 > v0 ? ((v1 - v0 + 1) / 2 + STRIDE - 1 - step0) / STRIDE : 0;
 
-        // The wave's next 32 steps, two tiles each, a lane per tile: where the tile lies, whether it is there, and whether all of the wave's
-        // rows see all of it.  One look at the table for 1024 tokens, and two instructions per tile to have its address.
+        // The wave's next 32 steps, two tiles each, a lane per tile: where the tile lies, whether it is there, and whether all rows see all of
+        // it.  One look at the table for 1024 tokens, and two instructions per tile to have its address.
         int64_t tile_at = 0;
         uint64_t there = 0, plain = 0;
-        auto tile_of = [&](int k, int u) {
-            const int v = v0 + 2 * (step0 + k * STRIDE) + u;
-            return v < sp.sinks ? v : v - sp.sinks + sp.lo;
-        };
+        auto tile_of = [&](int k, int u) { return listed_tile(sp, v0 + 2 * (step0 + k * STRIDE) + u); };
         auto look_up = [&](int k) {
             const int v = v0 + 2 * (step0 + (k + (lane >> 1)) * STRIDE) + (lane & 1);
-            const int tile = v < sp.sinks ? v : v - sp.sinks + sp.lo;
+            const int tile = listed_tile(sp, v);
             const int slot = tile >> kv.tile_shift;
             const int id = v < v1 && slot < kv.max_pages ? table[slot] : -1;
             const bool ok = id >= 0 && id < kv.n_pages;
             tile_at = (ok ? id : 0) * kv.page_bytes + (tile & tile_mask) * kv_tile_bytes(D);
             there = __ballot(ok);
-            plain = __ballot(ok && tile * 16 + 15 <= see_first && (a.window == 0 || tile * 16 > see_last - a.window || tile * 16 + 15 < a.sinks));
+            plain = __ballot(ok && b.all_see(a, tile));
+        };
+        auto tile_ptr = [&](int k, int u) {
+            const int l = 2 * (k & 31) + u;
+            const uint32_t lo = __builtin_amdgcn_readlane((int)tile_at, l), hi = __builtin_amdgcn_readlane((int)(tile_at >> 32), l);
+            return pool + ((uint64_t)hi << 32 | lo);
         };
         auto load_step = [&](int k, Piece<D> (&x)[2]) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int l = 2 * (k & 31) + u;
-                const uint32_t lo = __builtin_amdgcn_readlane((int)tile_at, l), hi = __builtin_amdgcn_readlane((int)(tile_at >> 32), l);
-                load_piece<D>(pool + ((uint64_t)hi << 32 | lo), g, n, x[u]);
+                const uint8_t *tile = tile_ptr(k, u);
+                load_keys<D>(tile, g, n, x[u]);
+                load_values<D>(tile, g, n, x[u]);
             }
         };
-        // what the loads of a step need to be told of it: whether its tiles are there, and plain (two bits each)
+        // of a step: whether its tiles are there, and plain (two bits each)
         auto flags_of = [&](int k) { return (uint32_t)(there >> (2 * (k & 31)) & 3u) | (uint32_t)(plain >> (2 * (k & 31)) & 3u) << 2; };
 
         auto step = [&](Piece<D> (&x)[2], uint32_t flags, int k) {
-            // scores, not scaled yet
-            f32x4 s[NQ][2];
+            uint4 kf[2][KI];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint4 kf[KI];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int j = 0; j < KI; ++j) {
-                    const float power = __uint_as_float((D == 256 ? (j >= KI / 2 ? x[u].k_power >> 8 : x[u].k_power & 255u) : x[u].k_power) << 23);
-                    kf[j] = make_uint4(two<0>(x[u].k[j], power), two<1>(x[u].k[j], power), two<2>(x[u].k[j], power), two<3>(x[u].k[j], power));
-                }
-#pragma unroll
-                for (int t = 0; t < NQ; ++t) {
-                    f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < KI; ++j) {
-                        c = mfma(kf[j], qf[t][j], c);
-                        if constexpr (HALF) c = mfma(kf[j], ql[t][j], c);
-                    }
-                    s[t][u] = c;
-                }
-            }
-
-            uint64_t odd[2] = {0, 0};   // lanes of values that hold a block without a finite power
-            if (flags != 15u) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bool page = flags >> u & 1u;
-                    const int j0 = tile_of(k, u) * 16 + 4 * g;
-#pragma unroll
-                    for (int t = 0; t < NQ; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int j = j0 + i;
-                            const bool sees = page && j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
-                            s[t][u][i] = sees ? s[t][u][i] : MINUS_INF;
-                        }
-                    // values: powers of tokens behind the last one, and of blocks that are NaN, count as the smallest
-                    uint32_t keep = 0;
-                    bool nan = false;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t b = (x[u].v_power >> (8 * i)) & 255u;
-                        const bool in = page && j0 + i <= see_last;
-                        keep |= in && b < 254u ? b << (8 * i) : 0u;
-                        nan = nan || (in && b >= 254u);
-                    }
-                    odd[u] = __ballot(nan);
-                    if (!nan) x[u].v_power = keep;
-                }
-            }
-
-            // running maximum, p, sum
+                for (int j = 0; j < KI; ++j) kf[u][j] = k_operand(x[u].k[j], k_power_of<D>(x[u].k_power, j));
             uint4 pf[NQ], pl[HALF ? NQ : 1];
 #pragma unroll
             for (int t = 0; t < NQ; ++t) {
-                float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
-                                  fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-                if (__any(top * a.scale > m[t] + 8.0f)) {
-                    top = fmaxf(top, __shfl_xor(top, 16, 64));
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float grown = fmaxf(m[t], top * a.scale);
-                    const float shrink = m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(m[t] - grown);
-                    m[t] = grown;
-                    l[t] *= shrink;
+                f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};   // scores, not scaled yet
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) o[t][i] *= shrink;
+                for (int j = 0; j < KI; ++j) {
+                    s[0] = mfma(kf[0][j], b.qf[t][j], s[0]);
+                    s[1] = mfma(kf[1][j], b.qf[t][j], s[1]);
+                    if constexpr (HALF) {
+                        s[0] = mfma(kf[0][j], b.ql[t][j], s[0]);
+                        s[1] = mfma(kf[1][j], b.ql[t][j], s[1]);
+                    }
                 }
-                const float ref = m[t] == MINUS_INF ? 0.0f : m[t];
-                float p[8];
+                if (flags != 15u) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][0][i], a.scale, -ref));
-                    p[4 + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][1][i], a.scale, -ref));
+                    for (int u = 0; u < 2; ++u) b.mask(a, s, t, u, flags >> u & 1u, tile_of(k, u) * 16 + 4 * g);
                 }
-                l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                uint32_t hi[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) hi[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-                pf[t] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                if constexpr (HALF) {
-                    uint32_t lo[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) lo[i] = pack_bf16(p[2 * i] - low(hi[i]), p[2 * i + 1] - high(hi[i]));
-                    pl[t] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                }
+                b.weigh(a, t, s, pf[t], pl[HALF ? t : 0]);
             }
-
-            if (__builtin_expect((odd[0] | odd[1]) != 0, 0)) {
-                // Blocks that are NaN in a step that not all rows see: they reach the rows that see them and no others.  A lane of O^T holds
-                // the sixteenths 4 g .. 4 g + 3 of row n, the power of which lies with lane (quad, sixteenth)
+            uint64_t bad[2] = {0, 0};   // lanes of values that hold a block without a finite power
+            uint32_t raw[2] = {0, 0};
+            if (flags != 15u) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-#pragma unroll 1
-                    for (int quad = 0; quad < 4; ++quad)
-#pragma unroll 1
-                        for (int i = 0; i < 4; ++i) {
-                            const int j = tile_of(k, u) * 16 + 4 * quad + i;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const uint32_t w = (uint32_t)__shfl((int)x[u].v_power, quad * 16 + 4 * g + e, 64);
-                                const bool bad = (flags >> u & 1u) && j <= see_last && ((w >> (8 * i)) & 255u) >= 254u;
-#pragma unroll
-                                for (int t = 0; t < NQ; ++t) {
-                                    const bool sees = bad && j <= pos[t] && (a.window == 0 || j > pos[t] - a.window || j < a.sinks);
-#pragma unroll
-                                    for (int c = 0; c < NI; ++c)
-                                        if (sees) o[t][c][e] = __builtin_nanf("");
-                                }
-                            }
-                        }
-                    uint32_t keep = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t b = (x[u].v_power >> (8 * i)) & 255u;
-                        keep |= b < 254u ? b << (8 * i) : 0u;
-                    }
-                    x[u].v_power = keep;
+                    bool nan;
+                    raw[u] = x[u].v_power;
+                    x[u].v_power = guard_values(x[u].v_power, flags >> u & 1u, tile_of(k, u) * 16 + 4 * g, b.see_last, nan);
+                    bad[u] = __ballot(nan);
                 }
             }
-
-            // outputs: token i of the lane's eight is token i % 4 of tile i / 4
+            if (__builtin_expect((bad[0] | bad[1]) != 0, 0)) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) b.spoil(a, raw[u], flags >> u & 1u, tile_of(k, u) * 16);
+            }
             float power[8];
+            powers(x[0].v_power, power);
+            powers(x[1].v_power, power + 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int sh = 8 * (i & 3);
-                const uint32_t vp = x[i >> 2].v_power;
-                power[i] = __uint_as_float(sh == 24 ? vp >> 1 & 0x7f800000u : vp << (23 - sh) & 0x7f800000u);
-            }
-#pragma unroll
-            for (int c = 0; c < NI / 2; ++c) {   // codes 2 c, 2 c + 1 of the lane's sixteenth
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int byte = (i & 3) * (D / 32) + c;
-                    w[i] = two_at(x[i >> 2].v[byte >> 2], power[i], byte & 3);
-                }
-                uint4 even, second;
-                even = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
-                                  __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u));
-                second = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u),
-                                    __builtin_amdgcn_perm(w[5], w[4], 0x07060302u), __builtin_amdgcn_perm(w[7], w[6], 0x07060302u));
+            for (int c = 0; c < NI / 2; ++c) {
+                uint4 even, odd;
+                v_operands<D>(x[0].v, x[1].v, power, c, even, odd);
 #pragma unroll
                 for (int t = 0; t < NQ; ++t) {
-                    o[t][2 * c] = mfma(even, pf[t], o[t][2 * c]);
-                    o[t][2 * c + 1] = mfma(second, pf[t], o[t][2 * c + 1]);
+                    b.o[t][2 * c] = mfma(even, pf[t], b.o[t][2 * c]);
+                    b.o[t][2 * c + 1] = mfma(odd, pf[t], b.o[t][2 * c + 1]);
                     if constexpr (HALF) {
-                        o[t][2 * c] = mfma(even, pl[t], o[t][2 * c]);
-                        o[t][2 * c + 1] = mfma(second, pl[t], o[t][2 * c + 1]);
+                        b.o[t][2 * c] = mfma(even, pl[t], b.o[t][2 * c]);
+                        b.o[t][2 * c + 1] = mfma(odd, pl[t], b.o[t][2 * c + 1]);
                     }
                 }
             }
@@ -424,105 +494,76 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             if (k + 2 < steps) load_step(k + 2, xa);
             if (k + 1 < steps) step(xb, fb, k + 1);
         }
+        b.end();
 
-        // sums over the four lanes of a row
-#pragma unroll
-        for (int t = 0; t < NQ; ++t) {
-            l[t] += __shfl_xor(l[t], 16, 64);
-            l[t] += __shfl_xor(l[t], 32, 64);
-        }
-
-        const bool whole = sp.parts == 1;
-        const int64_t all_rows = a.Qt * kv.n_heads * a.group;
-        // numbers [at, at + 4) of a row of the output
-        auto put4 = [&](int64_t row, int head, int d, const float (&y)[4]) {
-            if (whole) {
-                uint2 z;
-                if constexpr (HALF) z = make_uint2(f32_to_f16_bits(y[0]) | f32_to_f16_bits(y[1]) << 16, f32_to_f16_bits(y[2]) | f32_to_f16_bits(y[3]) << 16);
-                else z = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.out_token + head * a.out_head + d) = z;
-            } else {
-                float *dst = a.part_out + ((at.part * all_rows) + row * (kv.n_heads * a.group) + head) * D + d;
-                *reinterpret_cast<float4 *>(dst) = make_float4(y[0], y[1], y[2], y[3]);
-            }
-        };
-        auto put_stat = [&](int64_t row, int head, float mm, float ll) {
-            const int64_t i = row * (kv.n_heads * a.group) + head;
-            if (whole) {
-                if (a.lse) a.lse[i] = ll == 0.0f ? MINUS_INF : (mm + __builtin_amdgcn_logf(ll)) * 0.69314718055994531f;
-            } else {
-                a.part_stat[(at.part * all_rows + i) * 2] = mm;
-                a.part_stat[(at.part * all_rows + i) * 2 + 1] = ll;
-            }
-        };
+        const Sink<D, HALF> sink(kv, a, at.part, sp.parts == 1);
         if constexpr (ROWS) {
 #pragma unroll
             for (int t = 0; t < NQ; ++t) {
-                if (w_a + t * 16 + n > row_b) continue;
-                const float f = whole ? (l[t] == 0.0f ? 0.0f : 1.0f / l[t]) : 1.0f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int c = 0; c < NI; c += 4) {
-                        const float y[4] = {o[t][c][e] * f, o[t][c + 1][e] * f, o[t][c + 2][e] * f, o[t][c + 3][e] * f};
-                        put4(q_row[t], q_head[t], (4 * g + e) * NI + c, y);
-                    }
-                if (g == 0) put_stat(q_row[t], q_head[t], m[t], l[t]);
-            }
-        } else {
-            // the four waves' sums meet in LDS, one tile of 16 rows at a time
-            constexpr int LD = D + 4;
-            float *so = reinterpret_cast<float *>(smem);                       // [4][16][LD]
-            float *sm = so + 4 * 16 * LD, *sl = sm + 4 * RW;                   // [4][RW]
-            __syncthreads();
-            if (g == 0) {
-#pragma unroll
-                for (int t = 0; t < NQ; ++t) {
-                    sm[wave * RW + t * 16 + n] = m[t];
-                    sl[wave * RW + t * 16 + n] = l[t];
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < NQ; ++t) {
-                if (row_a + t * 16 > row_b) break;
-                __syncthreads();
-                float big = MINUS_INF;
-                for (int w = 0; w < 4; ++w) big = fmaxf(big, sm[w * RW + t * 16 + n]);
-                const float f = m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(m[t] - big);
+                const int row = row_a + wave * RW + t * 16 + n;
+                if (row > row_b) continue;
+                const int i = row / a.group, head = at.h * a.group + row - i * a.group;
+                const float f = sink.whole ? (b.l[t] == 0.0f ? 0.0f : 1.0f / b.l[t]) : 1.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int c = 0; c < NI; c += 4)
-                        *reinterpret_cast<float4 *>(so + (wave * 16 + n) * LD + (4 * g + e) * NI + c) =
-                            make_float4(o[t][c][e] * f, o[t][c + 1][e] * f, o[t][c + 2][e] * f, o[t][c + 3][e] * f);
-                __syncthreads();
-                // 16 threads per row
-                const int row = threadIdx.x >> 4, i16 = threadIdx.x & 15;
-                const int at_row = row_a + t * 16 + row;
-                if (at_row <= row_b) {
-                    float mm = MINUS_INF, ll = 0.0f;
-                    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w * RW + t * 16 + row]);
-                    for (int w = 0; w < 4; ++w) {
-                        const float mw = sm[w * RW + t * 16 + row];
-                        ll += mw == MINUS_INF ? 0.0f : sl[w * RW + t * 16 + row] * __builtin_amdgcn_exp2f(mw - mm);
-                    }
-                    const float fin = whole ? (ll == 0.0f ? 0.0f : 1.0f / ll) : 1.0f;
-                    const int i = at_row / a.group, head = at.h * a.group + at_row - i * a.group;
-#pragma unroll
-                    for (int c = 0; c < D; c += 64) {
-                        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        for (int w = 0; w < 4; ++w) {
-                            const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + row) * LD + c + i16 * 4);
-                            y[0] += v.x, y[1] += v.y, y[2] += v.z, y[3] += v.w;
-                        }
-                        for (int e = 0; e < 4; ++e) y[e] *= fin;
-                        put4(rq.first + i, head, c + i16 * 4, y);
-                    }
-                    if (i16 == 0) put_stat(rq.first + i, head, mm, ll);
-                }
+                        sink.put4(rq.first + i, head, (4 * g + e) * NI + c, b.o[t][c][e] * f, b.o[t][c + 1][e] * f, b.o[t][c + 2][e] * f, b.o[t][c + 3][e] * f);
+                if (g == 0) sink.put_stat(rq.first + i, head, b.m[t], b.l[t]);
             }
-            __syncthreads();
+            continue;
         }
+        // the four waves' sums meet in LDS, one tile of 16 rows at a time
+        constexpr int LD = D + 4;
+        float *so = reinterpret_cast<float *>(smem);                       // [4][16][LD]
+        float *sm = so + 4 * 16 * LD, *sl = sm + 4 * RW;                   // [4][RW]
+        __syncthreads();
+        if (g == 0) {
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                sm[wave * RW + t * 16 + n] = b.m[t];
+                sl[wave * RW + t * 16 + n] = b.l[t];
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) {
+            if (row_a + t * 16 > row_b) break;
+            __syncthreads();
+            float big = MINUS_INF;
+            for (int w = 0; w < 4; ++w) big = fmaxf(big, sm[w * RW + t * 16 + n]);
+            const float f = b.m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(b.m[t] - big);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int c = 0; c < NI; c += 4)
+                    *reinterpret_cast<float4 *>(so + (wave * 16 + n) * LD + (4 * g + e) * NI + c) =
+                        make_float4(b.o[t][c][e] * f, b.o[t][c + 1][e] * f, b.o[t][c + 2][e] * f, b.o[t][c + 3][e] * f);
+            __syncthreads();
+            // 16 threads per row
+            const int row = threadIdx.x >> 4, i16 = threadIdx.x & 15;
+            const int at_row = row_a + t * 16 + row;
+            if (at_row <= row_b) {
+                float mm = MINUS_INF, ll = 0.0f;
+                for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w * RW + t * 16 + row]);
+                for (int w = 0; w < 4; ++w) {
+                    const float mw = sm[w * RW + t * 16 + row];
+                    ll += mw == MINUS_INF ? 0.0f : sl[w * RW + t * 16 + row] * __builtin_amdgcn_exp2f(mw - mm);
+                }
+                const float fin = sink.whole ? (ll == 0.0f ? 0.0f : 1.0f / ll) : 1.0f;
+                const int i = at_row / a.group, head = at.h * a.group + at_row - i * a.group;
+#pragma unroll
+                for (int c = 0; c < D; c += 64) {
+                    float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int w = 0; w < 4; ++w) {
+                        const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + row) * LD + c + i16 * 4);
+                        y[0] += v.x, y[1] += v.y, y[2] += v.z, y[3] += v.w;
+                    }
+                    sink.put4(rq.first + i, head, c + i16 * 4, y[0] * fin, y[1] * fin, y[2] * fin, y[3] * fin);
+                }
+                if (i16 == 0) sink.put_stat(rq.first + i, head, mm, ll);
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -584,31 +625,32 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, 
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <int D, int NQ, bool HALF, bool ROWS>
-hipError_t run(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
+template <class K>
+hipError_t run(K *kernel, int lds, const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
 {
-    const int64_t groups = ceil_div((int64_t)kv.R * kv.n_heads, 8) * 8 * plan.row_tiles;
-    const int lds = lds_bytes<D>(NQ, ROWS);
+    const int64_t groups = ceil_div((int64_t)kv.R * kv.n_heads, 8) * 8 * plan.row_tiles * plan.parts;
     if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_attention_kernel<D, NQ, HALF, ROWS>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    kv_attention_kernel<D, NQ, HALF, ROWS><<<(unsigned)(groups * plan.parts), 256, lds, stream>>>(kv, a);
-    if (plan.parts > 1) {
-        // four rows of a row tile per workgroup, if there are that many
-        const int most = (int)ceil_div(plan.rows < a.max_rows ? plan.rows : a.max_rows, 4);
-        kv_join_kernel<D, HALF><<<(unsigned)((int64_t)kv.R * kv.n_heads * plan.row_tiles * most), 256, 0, stream>>>(kv, a, plan.rows, most);
-    }
+    kernel<<<(unsigned)groups, 256, lds, stream>>>(kv, a);
     return hipGetLastError();
 }
 template <int D, bool HALF>
 hipError_t run_form(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
 {
-    if (plan.form == KV_FORM_TOKENS16) return run<D, 1, HALF, false>(kv, a, plan, stream);
-    if constexpr (D < 256)
-        if (plan.form == KV_FORM_TOKENS32) return run<D, 2, HALF, false>(kv, a, plan, stream);
-    return run<D, D == 256 ? 1 : 2, HALF, true>(kv, a, plan, stream);
+    constexpr int N = D == 256 ? 1 : 2;   // 32 rows a wave: not with 256 numbers a head, whose operands and sums do not fit the registers
+    hipError_t e;
+    if (plan.rows == 16) e = run(kv_attention_kernel<D, 1, HALF, false>, lds_bytes<D, 1, false>(), kv, a, plan, stream);
+    else if (plan.rows == 64 * N) e = run(kv_attention_kernel<D, N, HALF, true>, lds_bytes<D, N, true>(), kv, a, plan, stream);
+    else e = run(kv_attention_kernel<D, N, HALF, false>, lds_bytes<D, N, false>(), kv, a, plan, stream);
+    if (e == hipSuccess && plan.parts > 1) {
+        // four rows of a row tile per workgroup, if there are that many
+        const int most = (int)ceil_div(plan.rows < a.max_rows ? plan.rows : a.max_rows, 4);
+        kv_join_kernel<D, HALF><<<(unsigned)((int64_t)kv.R * kv.n_heads * plan.row_tiles * most), 256, 0, stream>>>(kv, a, plan.rows, most);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace
@@ -618,8 +660,8 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
 {
     KvAttentionPlan p;
     const int64_t rows = (max_q < 1 ? 1 : max_q) * group;
-    p.form = rows <= 16 ? KV_FORM_TOKENS16 : rows <= 32 && d < 256 ? KV_FORM_TOKENS32 : KV_FORM_ROWS;   // 32 rows of 256 numbers do not fit the registers
-    p.rows = p.form == KV_FORM_TOKENS16 ? 16 : p.form == KV_FORM_TOKENS32 ? 32 : d == 256 ? 64 : 128;
+    const int32_t wave_rows = rows <= 16 || d == 256 ? 16 : 32;
+    p.rows = rows <= 2 * wave_rows ? wave_rows : 4 * wave_rows;
     p.row_tiles = (int32_t)ceil_div(rows, p.rows);
     p.max_rows = (int32_t)(rows < 0x7fffffff ? rows : 0x7fffffff);
     // tokens that a row tile may see
@@ -631,7 +673,7 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     const int64_t tiles = ceil_div(seen, KV_TILE);
     const int64_t groups = R * n_heads * p.row_tiles;
     // three workgroups for each of the 256 CUs, which is what their registers allow, if the parts do not get shorter than two steps of each wave
-    const int64_t least = p.form == KV_FORM_ROWS ? 8 : 16;
+    const int64_t least = p.rows > wave_rows ? 8 : 16;
     int64_t parts = ceil_div(768, groups);
     if (parts > ceil_div(tiles, least)) parts = ceil_div(tiles, least);
     if (parts > MAX_PARTS) parts = MAX_PARTS;

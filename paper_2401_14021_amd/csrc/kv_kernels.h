@@ -68,9 +68,7 @@ struct KvAttentionPlan {
     int32_t rows;          // query rows of a workgroup
     int32_t max_rows;      // of a request and key/value head, as far as the host knows
     int32_t row_tiles, parts, part_tiles;
-    int32_t form;          // KV_FORM_*
 };
-enum { KV_FORM_TOKENS16 = 0, KV_FORM_TOKENS32 = 1, KV_FORM_ROWS = 2 };
 KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t max_q, int64_t max_len, int32_t window,
                                   int32_t sinks);
 hipError_t launch_kv_attention(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream);
