@@ -480,18 +480,21 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             }
         };
 
-        // two steps a turn, the loads of the next one under way during each: no register is moved
+        // Two steps a turn with registers of their own, so that none is moved; the loads of the step behind a step are under way during it.  More of them
+        // gain nothing: a wave that is alone on its SIMD takes 0.63 us a step, which are its instructions in a row (290 of about 5 cycles).
         Piece<D> xa[2], xb[2];
-        if (steps > 0) {
-            look_up(0);
-            load_step(0, xa);
-        }
+        uint32_t fa = 0, fb = 0;
+        auto request = [&](int k, Piece<D> (&to)[2], uint32_t &f) {
+            if (k >= steps) return;
+            if ((k & 31) == 0) look_up(k);
+            f = flags_of(k);
+            load_step(k, to);
+        };
+        request(0, xa, fa);
         for (int k = 0; k < steps; k += 2) {
-            const uint32_t fa = flags_of(k), fb = flags_of(k + 1);
-            if (k + 1 < steps) load_step(k + 1, xb);
+            request(k + 1, xb, fb);
             step(xa, fa, k);
-            if (((k + 2) & 31) == 0 && k + 2 < steps) look_up(k + 2);
-            if (k + 2 < steps) load_step(k + 2, xa);
+            request(k + 2, xa, fa);
             if (k + 1 < steps) step(xb, fb, k + 1);
         }
         b.end();
@@ -672,12 +675,20 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     }
     const int64_t tiles = ceil_div(seen, KV_TILE);
     const int64_t groups = R * n_heads * p.row_tiles;
-    // three workgroups for each of the 256 CUs, which is what their registers allow, if the parts do not get shorter than two steps of each wave
-    const int64_t least = p.rows > wave_rows ? 8 : 16;
-    int64_t parts = ceil_div(768, groups);
-    if (parts > ceil_div(tiles, least)) parts = ceil_div(tiles, least);
-    if (parts > MAX_PARTS) parts = MAX_PARTS;
-    p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);
+    // Parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join and what every part does once.
+    // So nothing is split that fills the chip's 256 CUs as it is, or has no more than 8 steps a wave; else so that the workgroups are just one, two or three per CU
+    // (one more than that is a round of its own), more of them where parts stay long.  us in a graph, one to 48 contexts, unsplit, best, this rule: 32 heads x
+    // 640 tokens 7.9, 7.9, 7.9; x 2048 15.0, 9.7, 9.7; 8 x 4 heads x 32768 188, 18.2, 18.2; 16 requests of 8 x 4 x 2000 17.3, 14.7, 14.7; 64 of them
+    // 26.8 (33 in two parts); 6 x 115000 756, 144, 144.
+    int64_t parts = 1;
+    if (groups < 256 && tiles * d > 64 * 128) {
+        const int64_t one = 256 / groups, two = 512 / groups, three = 768 / groups;
+        parts = three <= MAX_PARTS && tiles >= three * 128 ? three : two <= 16 && tiles >= two * 24 ? two : one;
+        if (parts > tiles / 16) parts = tiles / 16;
+        if (parts > MAX_PARTS) parts = MAX_PARTS;
+        if (parts < 1) parts = 1;
+    }
+    p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);   // a step of every wave
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);
     return p;
 }
