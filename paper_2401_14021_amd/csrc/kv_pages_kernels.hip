@@ -4,9 +4,11 @@
 // page is free is its count alone, and the free page that is taken is always the lowest one, so the state after a call depends on nothing but the
 // state before it: counts change by whole-number atomics whose order cannot show, and nothing is a stack.
 //
-//  reserve   the k-th page needed (requests in order) is the k-th lowest free one: counts per block of pages and needs per request
+//  reserve   the k-th page needed (requests in order) is the k-th lowest free one.  Pools of up to 65536 pages and 1024 requests: one
+//            workgroup ranks and hands out (reserve_small_kernel).  Larger: counts per block of pages and needs per request
 //            (count_kernel), ranks from both (free_kernel), then every request takes its own (take_kernel).
-//  compact   n pages are in use; those behind place n (movers, in order) take the free places in front of it (holes, in order).
+//  compact   n pages are in use; those behind place n (movers, in order) take the free places in front of it (holes, in order).  Ranks
+//            likewise, by one workgroup (movers_small_kernel) or two launches.
 //
 // What bounds them: launches and chains of loads (a few microseconds each) for the whole numbers, memory for the pages themselves, whose copies share out
 // pieces of 16 KB over the chip.
@@ -191,6 +193,99 @@ __global__ __launch_bounds__(256) void take_kernel(KvPages kv, const int32_t *gr
     if (lane == 0) kv.lens[r] = (int32_t)(len + grow[r]);
 }
 
+// The same by one workgroup: a request per thread, neighbouring pages per thread.  16384 pages and 256 requests of which 128 grow: 16 us for the three launches
+// above and their two gaps of 1.5 us, 14.5 us (loads that follow from each other: lengths, last pages, their counts, the list, the table).
+constexpr int SMALL_PAGES = 65536, SMALL_REQUESTS = 1024;
+// which of the pages base .. base + per - 1 (per <= 64) are free, sixteen counts' loads under way at once; `between` is done while the first of them are
+template <class F>
+__device__ __forceinline__ uint64_t free_pages(const KvPages &kv, int base, int per, F between)
+{
+    uint64_t bits = 0;
+    for (int i0 = 0; i0 < per; i0 += 16) {
+        int c[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = i0 + i < per && base + i0 + i < kv.n_pages ? kv.refs[base + i0 + i] : 1;
+        if (i0 == 0) between();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bits |= (uint64_t)(c[i] <= 0) << (i0 + i);
+    }
+    return bits;
+}
+// the sums of v's two halves over the threads in front of this one, and over all 1024
+__device__ __forceinline__ u64 pair_before(u64 v, u64 *red, u64 &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 incl = v;
+    for (int s = 1; s < 64; s <<= 1) {
+        const u64 up = (u64)(uint32_t)__shfl_up((int)(uint32_t)(incl >> 32), s, 64) << 32 | (uint32_t)__shfl_up((int)(uint32_t)incl, s, 64);
+        if (lane >= s) incl += up;
+    }
+    if (lane == 63) red[wave] = incl;
+    __syncthreads();
+    u64 before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        before += w < wave ? red[w] : 0;
+        total += red[w];
+    }
+    return before + incl - v;
+}
+__global__ __launch_bounds__(1024) void reserve_small_kernel(KvPages kv, const int32_t *grow, int32_t *granted, int32_t *scratch)
+{
+    __shared__ u64 red[16];
+    __shared__ int s_first[SMALL_REQUESTS], s_place[SMALL_REQUESTS], n_pairs, s_taken;
+    const Scratch s = carve(scratch, kv.n_pages, kv.R);
+    const int r = threadIdx.x;
+    if (r == 0) n_pairs = s_taken = 0;
+    int word = 0;
+    const int per = (kv.n_pages + 1023) / 1024, base = r * per;
+    uint64_t bits = free_pages(kv, base, per, [&] { word = r < kv.R ? need_of(kv, grow, r) : 0; });
+    const int need = word < 0 ? 0 : word & ~NEED_COPY;
+    u64 total;
+    const u64 before = pair_before((u64)__popcll(bits) << 32 | (uint32_t)need, red, total);
+    const int n_free = (int)(total >> 32), wanted = (int)(uint32_t)total, first = (int)(uint32_t)before;
+    int rank = (int)(before >> 32);
+    for (; bits && rank < wanted; bits &= bits - 1, ++rank) s.list[rank] = base + __builtin_ctzll(bits);
+    const bool ok = word >= 0 && (need == 0 || first + need <= n_free);
+    if (ok && need) atomicMax(&s_taken, first + need);   // requests that are served come first, but for those that need nothing
+    const bool copy = word >= 0 && (word & NEED_COPY);
+    const int T = kv.page_tokens;
+    int64_t len = 0;
+    if (r < kv.R) len = clamped_len(kv.lens[r], (int64_t)kv.max_pages * T);
+    s_first[r] = first;
+    s_place[r] = (int)((len + T - 1) / T) * 2 - (copy ? 1 : 0);   // place behind the last page; odd: the page in front of it is copied
+    __syncthreads();
+    const int taken = s_taken;
+    for (int i = threadIdx.x; i < taken; i += 1024) {
+        // the last request whose first page is not behind page i is the one that needs it
+        int lo = 0, hi = kv.R - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (s_first[mid] <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        const int32_t page = s.list[i];
+        const int place = s_place[lo], nth = i - s_first[lo];
+        int32_t *at = kv.table + (int64_t)lo * kv.max_pages + (place >> 1) + nth;
+        if ((place & 1) && nth == 0) {
+            const int32_t old = *at;
+            const int k = atomicAdd(&n_pairs, 1);   // copies do not depend on each other: any order of the list will do
+            s.pairs[2 * k] = old;
+            s.pairs[2 * k + 1] = page;
+            atomicSub(&kv.refs[old], 1);
+        }
+        kv.refs[page] = 1;
+        *at = page;
+    }
+    if (r < kv.R) {
+        if (granted) granted[r] = ok;
+        if (ok && grow[r] > 0) kv.lens[r] = (int32_t)(len + grow[r]);
+    }
+    __syncthreads();
+    if (r == 0) *s.n_pairs = n_pairs;
+}
+
 __device__ __forceinline__ void copy_piece(uint8_t *pages, int64_t page_bytes, int32_t n_pages, int32_t src, int32_t dst, int64_t piece)
 {
     if (src < 0 || src >= n_pages || dst < 0 || dst >= n_pages || src == dst) return;
@@ -301,6 +396,36 @@ __global__ __launch_bounds__(256) void movers_kernel(KvPages kv, int32_t *scratc
     }
 }
 
+// the same by one workgroup, without count_kernel
+__global__ __launch_bounds__(1024) void movers_small_kernel(KvPages kv, int32_t *scratch, int32_t *used_out)
+{
+    __shared__ int red[16];
+    const Scratch s = carve(scratch, kv.n_pages, kv.R);
+    const int per = (kv.n_pages + 1023) / 1024, base = threadIdx.x * per;
+    const uint64_t bits = free_pages(kv, base, per, [] {});
+    const int mine = __popcll(bits);
+    const int before = sum_before<1024>(mine, red), used = kv.n_pages - group_sum<1024>(mine, red);
+    const int in_front = used <= base ? 0 : used - base >= 64 ? 64 : used - base;   // of this thread's pages, those in front of place `used`
+    const int holes = group_sum<1024>(__popcll(in_front == 64 ? bits : bits & ((1ull << in_front) - 1ull)), red);
+    if (threadIdx.x == 0) {
+        s.n_pairs[0] = holes;
+        *used_out = used;
+    }
+    int32_t *place = s.list, *hole = s.list + kv.n_pages, *mover = hole + kv.n_pages;
+    for (int i = 0; i < per && base + i < kv.n_pages; ++i) {
+        const int id = base + i, f = before + __popcll(bits & ((1ull << i) - 1ull));   // free pages in front of id
+        const bool is_free = bits >> i & 1u;
+        if (id < used) {
+            if (is_free) hole[f] = id;
+        } else if (!is_free) {
+            const int k = id - f - (used - holes);
+            place[id] = k;
+            mover[k] = id;
+            s.pairs[k] = kv.refs[id];
+        }
+    }
+}
+
 // tables and counts of the new order, and the copies
 __global__ __launch_bounds__(256) void move_kernel(KvPages kv, int32_t *scratch, const int32_t *used_in, int32_t *table_out, int32_t *refs_out)
 {
@@ -342,9 +467,13 @@ size_t kv_pages_scratch_words(int64_t n_pages, int64_t R)
 hipError_t launch_kv_reserve(const KvPages &kv, const int32_t *grow, int32_t *granted, int32_t *scratch, hipStream_t stream)
 {
     const Scratch s = carve(scratch, kv.n_pages, kv.R);
-    count_kernel<<<s.n_blocks + s.n_groups, 256, 0, stream>>>(kv, grow, scratch);
-    free_kernel<<<s.n_blocks, 256, 0, stream>>>(kv, scratch);
-    take_kernel<<<(kv.R + 3) / 4, 256, 0, stream>>>(kv, grow, granted, scratch);
+    if (kv.n_pages <= SMALL_PAGES && kv.R <= SMALL_REQUESTS) {
+        reserve_small_kernel<<<1, 1024, 0, stream>>>(kv, grow, granted, scratch);
+    } else {
+        count_kernel<<<s.n_blocks + s.n_groups, 256, 0, stream>>>(kv, grow, scratch);
+        free_kernel<<<s.n_blocks, 256, 0, stream>>>(kv, scratch);
+        take_kernel<<<(kv.R + 3) / 4, 256, 0, stream>>>(kv, grow, granted, scratch);
+    }
     copy_kernel<<<COPY_GROUPS, 256, 0, stream>>>(kv.pages, kv.page_bytes, kv.n_pages, s.pairs, s.pairs + 1, 2, 0, s.n_pairs);
     return hipGetLastError();
 }
@@ -371,9 +500,12 @@ hipError_t launch_kv_copy_pages(const KvPages &kv, const int32_t *src, const int
 hipError_t launch_kv_compact(const KvPages &kv, int32_t *table_out, int32_t *refs_out, int32_t *used, int32_t *scratch, hipStream_t stream)
 {
     const Scratch s = carve(scratch, kv.n_pages, kv.R);
-    KvPages pages_only = kv;   // no needs are counted
-    count_kernel<<<s.n_blocks, 256, 0, stream>>>(pages_only, nullptr, scratch);
-    movers_kernel<<<s.n_blocks, 256, 0, stream>>>(kv, scratch, used);
+    if (kv.n_pages <= SMALL_PAGES) {
+        movers_small_kernel<<<1, 1024, 0, stream>>>(kv, scratch, used);
+    } else {
+        count_kernel<<<s.n_blocks, 256, 0, stream>>>(kv, nullptr, scratch);   // pages alone: no workgroup counts needs
+        movers_kernel<<<s.n_blocks, 256, 0, stream>>>(kv, scratch, used);
+    }
     move_kernel<<<COPY_GROUPS, 256, 0, stream>>>(kv, scratch, used, table_out, refs_out);
     return hipGetLastError();
 }

@@ -59,7 +59,8 @@ def check_reserve(B, kv, grow):
     return want[3]
 
 
-@pytest.mark.parametrize("R,max_pages,n_pages", [(1, 4, 3), (5, 8, 30), (70, 6, 300), (300, 30, 9000), (700, 20, 20000)])
+@pytest.mark.parametrize("R,max_pages,n_pages", [(1, 4, 3), (5, 8, 30), (70, 6, 300), (300, 30, 9000), (700, 20, 20000), (1024, 12, 65536), (1025, 9, 20000),
+                                                 (60, 700, 65537), (1300, 30, 70000)])
 def test_rounds_of_forks_reservations_and_rollbacks(B, R, max_pages, n_pages):
     rng = np.random.default_rng(R)
     kv = new_cache(B, R, max_pages, n_pages)
@@ -137,7 +138,8 @@ def test_copies_of_pages(B, shape):
 
 
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("R,n_pages,share", [(1, 1, 0.0), (3, 9, 0.5), (40, 1000, 0.3), (200, 4096, 0.2), (500, 13000, 0.5)])
+@pytest.mark.parametrize("R,n_pages,share", [(1, 1, 0.0), (3, 9, 0.5), (40, 1000, 0.3), (200, 4096, 0.2), (500, 13000, 0.5), (900, 65536, 0.1),
+                                             (900, 65537, 0.1), (3, 70001, 0.0)])
 def test_compact(B, R, n_pages, share, in_place):
     rng = np.random.default_rng(R)
     max_pages = max(1, n_pages // R)
