@@ -456,6 +456,8 @@ class KVCache:
         self.n_layers, self.n_heads, self.d, self.page_tokens = n_layers, n_heads, d, page_tokens
         self.desc = ralm_kv_t(pages.data_ptr(), refs.numel(), n_layers, n_heads, d, page_tokens, table.data_ptr(), lens.data_ptr(),
                               refs.data_ptr(), table.shape[0], table.shape[1])
+        self._ref = ctypes.byref(self.desc)
+        self._heads, self._offsets = (n_heads, d), (table.shape[0] + 1,)   # shapes that every call compares with
 
     @classmethod
     def empty(cls, R: int, max_tokens: int, n_pages: int, *, n_layers: int, n_heads: int, d: int, page_tokens: int = 32,
@@ -476,17 +478,16 @@ def ralm_kv_page_bytes(n_layers: int, n_heads: int, d: int, page_tokens: int) ->
 
 
 def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor):
-    assert k.shape == v.shape and k.dim() == 3 and k.shape[1:] == (kv.n_heads, kv.d) and k.dtype == v.dtype
-    assert k.stride(2) == 1 and v.stride(2) == 1
-    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape[0] == kv.lens.shape[0] + 1
-    return k.stride(0), k.stride(1), v.stride(0), v.stride(1)
+    ks, vs = k.stride(), v.stride()
+    assert k.shape == v.shape and k.shape[1:] == kv._heads and k.dtype == v.dtype and len(ks) == 3 and ks[2] == vs[2] == 1
+    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape == kv._offsets
+    return ks[0], ks[1], vs[0], vs[1]
 
 
 def ralm_kv_append(kv: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor) -> None:
     """``k``, ``v`` [n, n_heads, d]: the last tokens of every request (room for them has been reserved)."""
     st = _kv_rows(kv, k, v, offsets)
-    _check(lib().ralm_kv_append(ctypes.byref(kv.desc), layer, k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, offsets.data_ptr(),
-                                k.shape[0], _stream()))
+    _check(lib().ralm_kv_append(kv._ref, layer, k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, offsets.data_ptr(), k.shape[0], _stream()))
 
 
 def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: Optional[torch.Tensor] = None,
@@ -498,15 +499,14 @@ def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: 
     if v is None:
         v = torch.empty(n, kv.n_heads, kv.d, dtype=k.dtype, device=kv.pages.device)
     st = _kv_rows(kv, k, v, offsets)
-    assert k.shape[0] == n and (start is None or (start.dtype == torch.int32 and start.shape == kv.lens.shape))
-    _check(lib().ralm_kv_read(ctypes.byref(kv.desc), layer, offsets.data_ptr(), n, _ptr(start), k.data_ptr(), v.data_ptr(),
-                              _DT[k.dtype], *st, _stream()))
+    assert k.shape[0] == n and (start is None or (start.dtype == torch.int32 and start.shape == kv.lens.shape and start.is_contiguous()))
+    _check(lib().ralm_kv_read(kv._ref, layer, offsets.data_ptr(), n, _ptr(start), k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, _stream()))
     return k, v
 
 
 def alloc_kv_attention_workspace(kv: KVCache, n_q_heads: int, Qt: int, max_q: int = 0, max_len: int = 0, window: int = 0,
                                  sinks: int = 0) -> torch.Tensor:
-    n = lib().ralm_kv_attention_workspace_bytes(ctypes.byref(kv.desc), n_q_heads, Qt, max_q, max_len, window, sinks)
+    n = lib().ralm_kv_attention_workspace_bytes(kv._ref, n_q_heads, Qt, max_q, max_len, window, sinks)
     if n == 0:
         raise RalmError(2, lib().ralm_last_error().decode())
     return torch.empty(int(n), dtype=torch.uint8, device=kv.pages.device)
@@ -516,26 +516,27 @@ def ralm_kv_attention(kv: KVCache, layer: int, q: torch.Tensor, offsets: torch.T
                       scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of every request's last tokens (``q`` [Qt, heads, d]) over its cache; ``scale`` None: d ** -0.5."""
-    assert q.dim() == 3 and q.shape[2] == kv.d and q.stride(2) == 1
-    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape[0] == kv.lens.shape[0] + 1
-    Qt, heads, d = q.shape
+    shape, qs = q.shape, q.stride()
+    Qt, heads, d = shape
+    assert d == kv.d and qs[2] == 1
+    assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape == kv._offsets
     if out is None:
-        out = torch.empty(Qt, heads, d, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1
-    assert lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous())
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    os_ = out.stride()
+    assert out.shape == shape and out.dtype == q.dtype and os_[2] == 1
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == shape[:2] and lse.is_contiguous())
     if q.dtype not in _DT:
         raise RalmError(4, f"dtype {q.dtype}")
     if workspace is None:
         workspace = alloc_kv_attention_workspace(kv, heads, Qt, max_q, max_len, window, sinks)
-    _check(lib().ralm_kv_attention(ctypes.byref(kv.desc), layer, q.data_ptr(), _DT[q.dtype], q.stride(0), q.stride(1), heads,
-                                   offsets.data_ptr(), Qt, max_q, max_len, d ** -0.5 if scale is None else float(scale), window, sinks,
-                                   out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), workspace.data_ptr(), workspace.numel(),
-                                   _stream()))
+    _check(lib().ralm_kv_attention(kv._ref, layer, q.data_ptr(), _DT[q.dtype], qs[0], qs[1], heads, offsets.data_ptr(), Qt, max_q,
+                                   max_len, d ** -0.5 if scale is None else float(scale), window, sinks, out.data_ptr(), os_[0],
+                                   os_[1], _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream()))
     return out
 
 
 def alloc_kv_pages_workspace(kv: KVCache) -> torch.Tensor:
-    n = int(lib().ralm_kv_pages_workspace_bytes(ctypes.byref(kv.desc)))
+    n = int(lib().ralm_kv_pages_workspace_bytes(kv._ref))
     return torch.empty(n, dtype=torch.uint8, device=kv.pages.device)
 
 
@@ -548,7 +549,7 @@ def ralm_kv_reserve(kv: KVCache, grow: torch.Tensor, workspace: Optional[torch.T
     if granted is None:
         granted = torch.empty_like(grow)
     assert granted.dtype == torch.int32 and granted.shape == grow.shape and granted.is_contiguous()
-    _check(lib().ralm_kv_reserve(ctypes.byref(kv.desc), grow.data_ptr(), granted.data_ptr(), workspace.data_ptr(), workspace.numel(),
+    _check(lib().ralm_kv_reserve(kv._ref, grow.data_ptr(), granted.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                  _stream()))
     return granted
 
@@ -557,18 +558,18 @@ def ralm_kv_fork(kv: KVCache, src: torch.Tensor, dst: torch.Tensor, keep: Option
     assert src.dtype == torch.int32 and dst.dtype == torch.int32 and src.shape == dst.shape and src.dim() == 1
     assert src.is_contiguous() and dst.is_contiguous()
     assert keep is None or (keep.dtype == torch.int32 and keep.shape == src.shape and keep.is_contiguous())
-    _check(lib().ralm_kv_fork(ctypes.byref(kv.desc), src.data_ptr(), dst.data_ptr(), _ptr(keep), src.shape[0], _stream()))
+    _check(lib().ralm_kv_fork(kv._ref, src.data_ptr(), dst.data_ptr(), _ptr(keep), src.shape[0], _stream()))
 
 
 def ralm_kv_truncate(kv: KVCache, new_lens: torch.Tensor) -> None:
     assert new_lens.dtype == torch.int32 and new_lens.shape == kv.lens.shape and new_lens.is_contiguous()
-    _check(lib().ralm_kv_truncate(ctypes.byref(kv.desc), new_lens.data_ptr(), _stream()))
+    _check(lib().ralm_kv_truncate(kv._ref, new_lens.data_ptr(), _stream()))
 
 
 def ralm_kv_copy_pages(kv: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
     assert src.dtype == torch.int32 and dst.dtype == torch.int32 and src.shape == dst.shape and src.dim() == 1
     assert src.is_contiguous() and dst.is_contiguous()
-    _check(lib().ralm_kv_copy_pages(ctypes.byref(kv.desc), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream()))
+    _check(lib().ralm_kv_copy_pages(kv._ref, src.data_ptr(), dst.data_ptr(), src.shape[0], _stream()))
 
 
 def ralm_kv_compact(kv: KVCache, table: Optional[torch.Tensor] = None, refs: Optional[torch.Tensor] = None,
@@ -582,7 +583,7 @@ def ralm_kv_compact(kv: KVCache, table: Optional[torch.Tensor] = None, refs: Opt
     used = torch.empty((), dtype=torch.int32, device=table.device)
     if workspace is None:
         workspace = alloc_kv_pages_workspace(kv)
-    _check(lib().ralm_kv_compact(ctypes.byref(kv.desc), table.data_ptr(), refs.data_ptr(), used.data_ptr(), workspace.data_ptr(),
+    _check(lib().ralm_kv_compact(kv._ref, table.data_ptr(), refs.data_ptr(), used.data_ptr(), workspace.data_ptr(),
                                  workspace.numel(), _stream()))
     return table, refs, used
 

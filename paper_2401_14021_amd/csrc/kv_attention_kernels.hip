@@ -354,17 +354,18 @@ struct Sink {
     }
 };
 
-// ROWS: each of a workgroup's four waves has NQ * 16 rows of its own and goes over all tokens of the part (many rows; the waves never wait for each
-// other).  Else all have the same NQ * 16 rows and share out the part's tokens, 32 at a time, and their sums meet in LDS (few rows).
-template <int D, int NQ, bool ROWS>
-constexpr int lds_bytes() { return ROWS ? 16 : 4 * 16 * (D + 4) * 4 + 2 * 4 * 16 * NQ * 4; }
+// ROWS: each of a workgroup's waves has NQ * 16 rows of its own and goes over all tokens of the part (many rows; the waves never wait for each
+// other).  Else all have the same NQ * 16 rows and share out the part's tokens, 32 at a time, and their sums meet in LDS (few rows).  Four waves, or eight
+// where there is at most a workgroup for every CU.
+template <int D, int NQ, bool ROWS, int WAVES>
+constexpr int lds_bytes() { return ROWS ? 16 : WAVES * 16 * (D + 4) * 4 + 2 * WAVES * 16 * NQ * 4; }
 
-template <int D, int NQ, bool HALF, bool ROWS>
-__global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttention a)
+template <int D, int NQ, bool HALF, bool ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void kv_attention_kernel(KvView kv, KvAttention a)
 {
     using B = Block<D, NQ, HALF>;
-    constexpr int KI = B::KI, NI = B::NI, RW = NQ * 16, RG = ROWS ? 4 * RW : RW;   // rows of a wave, of the workgroup
-    constexpr int STRIDE = ROWS ? 1 : 4;                                              // a wave's steps are every STRIDE-th
+    constexpr int KI = B::KI, NI = B::NI, RW = NQ * 16, RG = ROWS ? WAVES * RW : RW;   // rows of a wave, of the workgroup
+    constexpr int STRIDE = ROWS ? 1 : WAVES;                                              // a wave's steps are every STRIDE-th
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
@@ -516,10 +517,10 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             }
             continue;
         }
-        // the four waves' sums meet in LDS, one tile of 16 rows at a time
-        constexpr int LD = D + 4;
-        float *so = reinterpret_cast<float *>(smem);                       // [4][16][LD]
-        float *sm = so + 4 * 16 * LD, *sl = sm + 4 * RW;                   // [4][RW]
+        // the waves' sums meet in LDS, one tile of 16 rows at a time
+        constexpr int LD = D + 4, TPR = WAVES * 4;                         // threads per row
+        float *so = reinterpret_cast<float *>(smem);                       // [WAVES][16][LD]
+        float *sm = so + WAVES * 16 * LD, *sl = sm + WAVES * RW;           // [WAVES][RW]
         __syncthreads();
         if (g == 0) {
 #pragma unroll
@@ -533,7 +534,8 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
             if (row_a + t * 16 > row_b) break;
             __syncthreads();
             float big = MINUS_INF;
-            for (int w = 0; w < 4; ++w) big = fmaxf(big, sm[w * RW + t * 16 + n]);
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) big = fmaxf(big, sm[w * RW + t * 16 + n]);
             const float f = b.m[t] == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(b.m[t] - big);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -542,28 +544,32 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvView kv, KvAttentio
                     *reinterpret_cast<float4 *>(so + (wave * 16 + n) * LD + (4 * g + e) * NI + c) =
                         make_float4(b.o[t][c][e] * f, b.o[t][c + 1][e] * f, b.o[t][c + 2][e] * f, b.o[t][c + 3][e] * f);
             __syncthreads();
-            // 16 threads per row
-            const int row = threadIdx.x >> 4, i16 = threadIdx.x & 15;
+            const int row = threadIdx.x / TPR, i0 = threadIdx.x % TPR;
             const int at_row = row_a + t * 16 + row;
             if (at_row <= row_b) {
                 float mm = MINUS_INF, ll = 0.0f;
-                for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w * RW + t * 16 + row]);
-                for (int w = 0; w < 4; ++w) {
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, sm[w * RW + t * 16 + row]);
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
                     const float mw = sm[w * RW + t * 16 + row];
                     ll += mw == MINUS_INF ? 0.0f : sl[w * RW + t * 16 + row] * __builtin_amdgcn_exp2f(mw - mm);
                 }
                 const float fin = sink.whole ? (ll == 0.0f ? 0.0f : 1.0f / ll) : 1.0f;
                 const int i = at_row / a.group, head = at.h * a.group + at_row - i * a.group;
 #pragma unroll
-                for (int c = 0; c < D; c += 64) {
+                for (int c0 = 0; c0 < D; c0 += 4 * TPR) {
+                    const int c = c0 + i0 * 4;
+                    if (4 * TPR > D && c >= D) continue;
                     float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    for (int w = 0; w < 4; ++w) {
-                        const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + row) * LD + c + i16 * 4);
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) {
+                        const float4 v = *reinterpret_cast<const float4 *>(so + (w * 16 + row) * LD + c);
                         y[0] += v.x, y[1] += v.y, y[2] += v.z, y[3] += v.w;
                     }
-                    sink.put4(rq.first + i, head, c + i16 * 4, y[0] * fin, y[1] * fin, y[2] * fin, y[3] * fin);
+                    sink.put4(rq.first + i, head, c, y[0] * fin, y[1] * fin, y[2] * fin, y[3] * fin);
                 }
-                if (i16 == 0) sink.put_stat(rq.first + i, head, mm, ll);
+                if (i0 == 0) sink.put_stat(rq.first + i, head, mm, ll);
             }
         }
         __syncthreads();
@@ -629,31 +635,37 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <class K>
-hipError_t run(K *kernel, int lds, const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
+hipError_t run(K *kernel, int waves, int lds, const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
 {
     const int64_t groups = ceil_div((int64_t)kv.R * kv.n_heads, 8) * 8 * plan.row_tiles * plan.parts;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    kernel<<<(unsigned)groups, 256, lds, stream>>>(kv, a);
+    kernel<<<(unsigned)groups, 64 * waves, lds, stream>>>(kv, a);
     return hipGetLastError();
 }
 template <int D, bool HALF>
 hipError_t run_form(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
 {
     constexpr int N = D == 256 ? 1 : 2;   // 32 rows a wave: not with 256 numbers a head, whose operands and sums do not fit the registers
-    hipError_t e;
-    if (plan.rows == 16) e = run(kv_attention_kernel<D, 1, HALF, false>, lds_bytes<D, 1, false>(), kv, a, plan, stream);
-    else if (plan.rows == 64 * N) e = run(kv_attention_kernel<D, N, HALF, true>, lds_bytes<D, N, true>(), kv, a, plan, stream);
-    else e = run(kv_attention_kernel<D, N, HALF, false>, lds_bytes<D, N, false>(), kv, a, plan, stream);
-    if (e == hipSuccess && plan.parts > 1) {
+    auto finish = [&](hipError_t e) {
+        if (e != hipSuccess || plan.parts == 1) return e;
         // four rows of a row tile per workgroup, if there are that many
         const int most = (int)ceil_div(plan.rows < a.max_rows ? plan.rows : a.max_rows, 4);
         kv_join_kernel<D, HALF><<<(unsigned)((int64_t)kv.R * kv.n_heads * plan.row_tiles * most), 256, 0, stream>>>(kv, a, plan.rows, most);
-        e = hipGetLastError();
+        return hipGetLastError();
+    };
+    constexpr bool EIGHT1 = D <= 128, EIGHT2 = D == 64 || (D == 128 && !HALF);   // eight waves: half the registers a wave
+    if (plan.rows == 64 * N) return finish(run(kv_attention_kernel<D, N, HALF, true, 4>, 4, lds_bytes<D, N, true, 4>(), kv, a, plan, stream));
+    if (plan.waves == 8) {
+        if constexpr (EIGHT1)
+            if (plan.rows == 16) return finish(run(kv_attention_kernel<D, 1, HALF, false, 8>, 8, lds_bytes<D, 1, false, 8>(), kv, a, plan, stream));
+        if constexpr (EIGHT2)
+            if (plan.rows == 32) return finish(run(kv_attention_kernel<D, 2, HALF, false, 8>, 8, lds_bytes<D, 2, false, 8>(), kv, a, plan, stream));
     }
-    return e;
+    if (plan.rows == 16) return finish(run(kv_attention_kernel<D, 1, HALF, false, 4>, 4, lds_bytes<D, 1, false, 4>(), kv, a, plan, stream));
+    return finish(run(kv_attention_kernel<D, N, HALF, false, 4>, 4, lds_bytes<D, N, false, 4>(), kv, a, plan, stream));
 }
 
 }  // namespace
@@ -675,16 +687,26 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     }
     const int64_t tiles = ceil_div(seen, KV_TILE);
     const int64_t groups = R * n_heads * p.row_tiles;
-    // Parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join and what every part does once.
-    // So nothing is split that fills the chip's 256 CUs as it is, or has no more than 8 steps a wave; else so that the workgroups are just one, two or three per CU
-    // (one more than that is a round of its own), more of them where parts stay long.  us in a graph, one to 48 contexts, unsplit, best, this rule: 32 heads x
-    // 640 tokens 7.9, 7.9, 7.9; x 2048 15.0, 9.7, 9.7; 8 x 4 heads x 32768 188, 18.2, 18.2; 16 requests of 8 x 4 x 2000 17.3, 14.7, 14.7; 64 of them
-    // 26.8 (33 in two parts); 6 x 115000 756, 144, 144.
+    // Waves and parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join, and what every part does once.
+    // So nothing is split that fills the chip's 256 CUs as it is or is short (80 tiles of 128 numbers).  Where there is at most a workgroup per CU
+    // it has eight waves, and parts make up one per CU; three of four waves each, which is what their registers allow, where parts stay long; with waves
+    // that have rows of their own, two or one.  One workgroup more than that would be a round of its own.
+    // us in a graph, 4 waves unsplit, 8 waves unsplit, best split: 1 context, 32 heads x 640 tokens 7.9, 7.8, 9.0; x 1280 -, 10.4, 10.2; x 2048 15.0, 13.2,
+    // 9.8; 8 x 4 heads x 32768 188, 135, 17.6; 32 requests, 8 x 8 heads, 4 drafts x 2000 26.4, 22.6, 30; 6 x 115000 756, -, 142 (16 parts of 4 waves; 8 of 8
+    // waves 148); 64 requests, 8 x 4 heads x 2000 26.8, -, 33.
+    const bool many = p.rows > wave_rows;
+    p.waves = 4;
     int64_t parts = 1;
-    if (groups < 256 && tiles * d > 64 * 128) {
+    if (groups < 256 || (groups == 256 && !many)) {
+        const bool is_short = tiles * d <= 80 * 128;
         const int64_t one = 256 / groups, two = 512 / groups, three = 768 / groups;
-        parts = three <= MAX_PARTS && tiles >= three * 128 ? three : two <= 16 && tiles >= two * 24 ? two : one;
-        if (parts > tiles / 16) parts = tiles / 16;
+        if (three <= MAX_PARTS && tiles >= three * 128) {
+            parts = three;
+        } else {
+            p.waves = many ? 4 : 8;
+            if (!is_short) parts = many && two <= 16 && tiles >= two * 24 ? two : one;
+        }
+        if (parts > tiles / 16) parts = tiles / 16;   // two steps of each of four waves
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         if (parts < 1) parts = 1;
     }

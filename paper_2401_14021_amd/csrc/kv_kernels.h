@@ -66,6 +66,7 @@ struct KvAttention {
 };
 struct KvAttentionPlan {
     int32_t rows;          // query rows of a workgroup
+    int32_t waves;         // of a workgroup
     int32_t max_rows;      // of a request and key/value head, as far as the host knows
     int32_t row_tiles, parts, part_tiles;
 };

@@ -67,11 +67,12 @@ def test_append_and_read(b):
 
 
 def test_attention(b):
-    L, kv = b.lib(), desc(b)
-    big = L.ralm_kv_attention_workspace_bytes(kv, 8, 4, 1, 512, 0, 0)
-    assert big > 256                                                       # few requests: split
+    L, kv = b.lib(), desc(b, max_pages=256)
+    big = L.ralm_kv_attention_workspace_bytes(kv, 8, 4, 1, 8192, 0, 0)
+    assert big > 256                                                       # a few long contexts: split
+    assert L.ralm_kv_attention_workspace_bytes(kv, 8, 4, 1, 300, 0, 0) == 256
 
-    def at(layer=0, q=P, dt=1, qs=(0, 0), heads=8, off=P, Qt=4, mq=1, ml=512, scale=1.0, w=0, f=0, out=P, os_=(0, 0), ws=P, n=big):
+    def at(layer=0, q=P, dt=1, qs=(0, 0), heads=8, off=P, Qt=4, mq=1, ml=8192, scale=1.0, w=0, f=0, out=P, os_=(0, 0), ws=P, n=big):
         return L.ralm_kv_attention(kv, layer, q, dt, *qs, heads, off, Qt, mq, ml, scale, w, f, out, *os_, None, ws, n, None)
     assert at(q=None) == NULL and at(out=None) == NULL and at(off=None) == NULL
     assert at(layer=2) == RANGE and at(layer=-1) == RANGE and at(Qt=-1) == RANGE and at(mq=-1) == RANGE and at(ml=-1) == RANGE
