@@ -1,0 +1,77 @@
+"""The example generator: retrieval, speculation and the 4-bit cache together.  With a target so sharp that every draw takes its best token,
+speculation, forks, rollbacks and compaction must not change what is generated."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def ex():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    spec = importlib.util.spec_from_file_location("neighbour_generator", os.path.join(ROOT, "examples", "neighbour_generator.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def check_pages(kv):
+    table, lens, refs = (t.cpu().numpy() for t in (kv.table, kv.lens, kv.refs))
+    count = np.zeros_like(refs)
+    for r, n in enumerate(lens):
+        held = -(-int(n) // kv.page_tokens)
+        assert (table[r, :held] >= 0).all() and (table[r, held:] == -1).all()
+        np.add.at(count, table[r, :held], 1)
+    np.testing.assert_array_equal(count, refs)
+
+
+@pytest.mark.parametrize("window", [0, 48])
+def test_speculation_does_not_change_a_certain_text(ex, window):
+    texts = {}
+    for stride in (0, 3, 6):
+        # one request's draws do not depend on the others' here, so all are alike and the batch only shares the prompt's pages
+        gen = ex.Generator(ex.Decoder(window=window, sinks=3), requests=3, share=0.0, sharpness=1e4)
+        gen.prompt(gen.corpus[30:77])
+        accepted = 0
+        i = 0
+        while min(map(len, gen.texts)) < 40:
+            accepted += gen.round(stride)
+            check_pages(gen.kv)
+            i += 1
+            if i % 5 == 0:
+                used = gen.compact()
+                check_pages(gen.kv)
+                assert int((gen.kv.refs[:used] > 0).sum()) == used and int(gen.kv.refs[used:].sum()) == 0
+        assert (gen.kv.lens.cpu().numpy() == np.array([46 + len(t) for t in gen.texts])).all()   # the last token is not in the cache yet
+        texts[stride] = [t[:40] for t in gen.texts]
+        assert texts[stride][0] == texts[stride][1] == texts[stride][2]
+    assert texts[0] == texts[3] == texts[6]
+
+
+def test_neighbours_are_drafted_and_accepted(ex):
+    gen = ex.Generator(ex.Decoder(), requests=4, share=1.0, seed=5)       # the target is the neighbours' distribution alone
+    gen.prompt(gen.corpus[200:260])
+    drafted = accepted = 0
+    for i in range(12):
+        accepted += gen.round(3 if i else 0)
+        drafted += 12 if i else 0
+        check_pages(gen.kv)
+    assert all(0 <= t < gen.model.V for text in gen.texts for t in text)
+    assert 0 < accepted <= drafted
+    assert sum(map(len, gen.texts)) == 4 * 13 + accepted
+
+
+def test_requests_that_end_give_their_pages_back(ex):
+    from paper_2401_14021_amd import binding as B
+    gen = ex.Generator(ex.Decoder(), requests=4)
+    gen.prompt(gen.corpus[:64])
+    for i in range(4):
+        gen.round(2)
+    B.ralm_kv_truncate(gen.kv, torch.zeros(4, dtype=torch.int32, device="cuda"))
+    check_pages(gen.kv)
+    assert int(gen.kv.refs.sum()) == 0 and gen.compact() == 0
