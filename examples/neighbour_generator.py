@@ -83,8 +83,11 @@ class Generator:
         self.kv = model.cache(requests, max_tokens, requests * (max_tokens // 16) + 8)
         self.pages_ws = B.alloc_kv_pages_workspace(self.kv)
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
-        # the datastore: states of a corpus of random tokens, in chunks of a prompt's length, and what followed
-        tokens = torch.randint(0, model.V, (corpus,), generator=self.gen, device="cuda", dtype=torch.int32)
+        # the datastore: states of a corpus in which a phrase comes again and again, one token in ten another, and what followed
+        phrase = torch.randint(0, model.V, (97,), generator=self.gen, device="cuda", dtype=torch.int32)
+        tokens = phrase[torch.arange(corpus, device="cuda") % 97]
+        noise = torch.randint(0, model.V, (corpus,), generator=self.gen, device="cuda", dtype=torch.int32)
+        tokens = torch.where(torch.rand(corpus, generator=self.gen, device="cuda") < 0.1, noise, tokens)
         book = model.cache(1, corpus, corpus // 16)
         B.ralm_kv_reserve(book, torch.tensor([corpus], dtype=torch.int32, device="cuda"))
         states, _ = model.run(book, tokens, torch.arange(corpus, device="cuda"), torch.tensor([0, corpus], device="cuda"), corpus, corpus)

@@ -1,5 +1,6 @@
 """The example generator: retrieval, speculation and the 4-bit cache together.  With a target so sharp that every draw takes its best token,
-speculation, forks, rollbacks and compaction must not change what is generated."""
+whatever was drafted, forked, rolled back and compacted on the way, every token must be the one that the decoder prefers when it is given
+the whole text at once."""
 import importlib.util
 import os
 
@@ -30,27 +31,42 @@ def check_pages(kv):
     np.testing.assert_array_equal(count, refs)
 
 
+def worst_gap(ex, model, prompt, text):
+    """How far below the best logit the text's tokens are, with prompt and text run as one chunk through a cache of their own."""
+    from paper_2401_14021_amd import binding as B
+    tokens = torch.cat([prompt, torch.tensor(text[:-1], dtype=torch.int32, device="cuda")])
+    n = tokens.shape[0]
+    kv = model.cache(1, n, n // 16 + 1)
+    B.ralm_kv_reserve(kv, torch.tensor([n], dtype=torch.int32, device="cuda"))
+    _, logits = model.run(kv, tokens, torch.arange(n, device="cuda"), torch.tensor([0, n], device="cuda"), n, n)
+    logits = logits[len(prompt) - 1:]
+    taken = logits.gather(1, torch.tensor(text, device="cuda").unsqueeze(1)).squeeze(1)
+    return float((logits.amax(1) - taken).max())
+
+
 @pytest.mark.parametrize("window", [0, 48])
-def test_speculation_does_not_change_a_certain_text(ex, window):
-    texts = {}
-    for stride in (0, 3, 6):
-        # one request's draws do not depend on the others' here, so all are alike and the batch only shares the prompt's pages
-        gen = ex.Generator(ex.Decoder(window=window, sinks=3), requests=3, share=0.0, sharpness=1e4)
-        gen.prompt(gen.corpus[30:77])
-        accepted = 0
-        i = 0
-        while min(map(len, gen.texts)) < 40:
-            accepted += gen.round(stride)
+@pytest.mark.parametrize("stride", [0, 3, 6])
+def test_speculation_does_not_change_what_is_generated(ex, window, stride):
+    """Logits have a spread of 1 and the best of 512 lies some 0.3 above the next.  Two runs differ by the roundings of weights and outputs to
+    bf16 (2^-8) in two layers, a few hundredths at most; draws at a sharpness of 10000 take tokens up to 0.002 below the best.  A wrong context
+    misses by 1 and more.  The bound is 0.1."""
+    gen = ex.Generator(ex.Decoder(window=window, sinks=3), requests=3, share=0.0, sharpness=1e4)
+    prompt = gen.corpus[30:77]
+    gen.prompt(prompt)
+    accepted = i = 0
+    while min(map(len, gen.texts)) < 40:
+        accepted += gen.round(stride)
+        check_pages(gen.kv)
+        i += 1
+        if i % 5 == 0:
+            used = gen.compact()
             check_pages(gen.kv)
-            i += 1
-            if i % 5 == 0:
-                used = gen.compact()
-                check_pages(gen.kv)
-                assert int((gen.kv.refs[:used] > 0).sum()) == used and int(gen.kv.refs[used:].sum()) == 0
-        assert (gen.kv.lens.cpu().numpy() == np.array([46 + len(t) for t in gen.texts])).all()   # the last token is not in the cache yet
-        texts[stride] = [t[:40] for t in gen.texts]
-        assert texts[stride][0] == texts[stride][1] == texts[stride][2]
-    assert texts[0] == texts[3] == texts[6]
+            assert int((gen.kv.refs[:used] > 0).sum()) == used and int(gen.kv.refs[used:].sum()) == 0
+    assert (gen.kv.lens.cpu().numpy() == np.array([46 + len(t) for t in gen.texts])).all()   # the last token is not in the cache yet
+    for text in gen.texts:
+        assert worst_gap(ex, gen.model, prompt, text) < 0.1
+    # the measure sees a context that is wrong in one place
+    assert worst_gap(ex, gen.model, torch.roll(prompt, 1), gen.texts[0]) > 0.1
 
 
 def test_neighbours_are_drafted_and_accepted(ex):
