@@ -216,6 +216,7 @@ ralm_status ralm_kv_attention(const ralm_kv_t *kv, int32_t layer, const void *q,
     a.parts = plan.parts;
     a.part_tiles = plan.part_tiles;
     a.max_rows = plan.max_rows;
+    a.by_length = plan.by_length;
     a.part_out = static_cast<float *>(workspace);
     a.part_stat = plan.parts > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + out_bytes) : nullptr;
     return launched(launch_kv_attention(view_of(kv, layer), a, plan, static_cast<hipStream_t>(stream)));

@@ -130,21 +130,53 @@ __device__ __forceinline__ Request request_of(const KvView &kv, const KvAttentio
     return x;
 }
 
+// The request that is the rank-th longest (equal ones in their order), R <= 64, by all lanes of every wave; lds: 64 words, in which the waves write the same.
+// 64 comparisons of what 16 reads bring: with a read of a lane's register per request this took 2.5 us of a call.
+__device__ __forceinline__ int longest_request(const KvView &kv, int rank, uint32_t *lds)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const int32_t len = (int)lane < kv.R ? kv.lens[lane] : 0;
+    // no two alike; lanes without a request come last.  Beyond 2^25 tokens lengths count as equal
+    const uint32_t key = (uint32_t)(len < 0 ? 0 : len > 1 << 25 ? 1 << 25 : len) * 64u + (63u - lane);
+    lds[lane] = key;
+    uint32_t before = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const uint4 k = reinterpret_cast<const uint4 *>(lds)[j];
+        before += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+    }
+    return __builtin_ctzll(__ballot(before == (uint32_t)rank));
+}
+
 // A workgroup's place: the row tiles of a key/value head are neighbours on one XCD (workgroup b runs on XCD b % 8), whose L2 then holds what
 // they all read
 struct Place {
     int r, h, rt, part;
 };
-__device__ __forceinline__ Place place_of(const KvView &kv, const KvAttention &a, int parts)
+__device__ __forceinline__ Place place_of(const KvView &kv, const KvAttention &a, int parts, uint32_t *lds)
 {
     const uint32_t pairs = (uint32_t)kv.R * kv.n_heads, per = (uint32_t)a.row_tiles * parts;
     const uint32_t b = blockIdx.x, xcd = b & 7u, i = b >> 3;
     Place x;
-    const uint32_t pair = i / per * 8 + xcd, rest = i % per;
-    x.r = pair < pairs ? (int)(pair / kv.n_heads) : -1;
-    x.h = (int)(pair % kv.n_heads);
+    uint32_t pair = i / per * 8 + xcd;
+    const uint32_t rest = i % per;
     x.part = (int)(rest / a.row_tiles);
     x.rt = a.row_tiles - 1 - (int)(rest % a.row_tiles);   // the last rows see the most tokens: first
+    if (pair >= pairs) {
+        x.r = -1;
+        x.h = 0;
+        return x;
+    }
+    if (a.by_length) {
+        // A few workgroups per CU that start at once: 32 CUs of an XCD get the longest 32 in order, the next 32 in reverse, and so on, so that every CU
+        // has about as many tokens
+        const uint32_t n = (pairs - xcd + 7) / 8, round = i / 32 * 32, last = round + 32 < n ? round + 32 : n;
+        if (a.by_length == 1 && (i & 32u)) pair = (last - 1 - (i - round)) * 8 + xcd;   // 2: many rounds of workgroups, the longest first
+        x.r = longest_request(kv, (int)(pair / kv.n_heads), lds);
+    } else {
+        x.r = (int)(pair / kv.n_heads);
+    }
+    x.h = (int)(pair % kv.n_heads);
     return x;
 }
 
@@ -358,7 +390,7 @@ struct Sink {
 // other).  Else all have the same NQ * 16 rows and share out the part's tokens, 32 at a time, and their sums meet in LDS (few rows).  Four waves, or eight
 // where there is at most a workgroup for every CU.
 template <int D, int NQ, bool ROWS, int WAVES>
-constexpr int lds_bytes() { return ROWS ? 16 : WAVES * 16 * (D + 4) * 4 + 2 * WAVES * 16 * NQ * 4; }
+constexpr int lds_bytes() { return ROWS ? 256 : WAVES * 16 * (D + 4) * 4 + 2 * WAVES * 16 * NQ * 4; }
 
 template <int D, int NQ, bool HALF, bool ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void kv_attention_kernel(KvView kv, KvAttention a)
@@ -369,7 +401,7 @@ __global__ __launch_bounds__(64 * WAVES) void kv_attention_kernel(KvView kv, KvA
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
-    const Place at = place_of(kv, a, a.parts);
+    const Place at = place_of(kv, a, a.parts, reinterpret_cast<uint32_t *>(smem));
     if (at.r < 0) return;
     const Request rq = request_of(kv, a, at.r);
     const int rows = rq.count * a.group;
@@ -710,6 +742,7 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         if (parts < 1) parts = 1;
     }
+    p.by_length = R > 1 && R <= 64 && groups > 256 ? (p.row_tiles == 1 && !many ? 1 : 2) : 0;
     p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);   // a step of every wave
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);
     return p;

@@ -61,12 +61,14 @@ struct KvAttention {
     // the launch, from kv_attention_plan
     int32_t row_tiles, parts, part_tiles;
     int32_t max_rows;      // queries x group, as far as the host knows
+    int32_t by_length;     // 1: workgroups are handed out by the requests' lengths
     float *part_out;       // [parts][Qt * heads][d], sums that are not divided yet
     float *part_stat;      // [parts][Qt * heads][2], largest score and sum
 };
 struct KvAttentionPlan {
     int32_t rows;          // query rows of a workgroup
     int32_t waves;         // of a workgroup
+    int32_t by_length;
     int32_t max_rows;      // of a request and key/value head, as far as the host knows
     int32_t row_tiles, parts, part_tiles;
 };

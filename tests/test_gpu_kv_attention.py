@@ -211,6 +211,25 @@ def test_long_contexts_in_parts(B, Hq, s):
         check_attention(B, [4000, 900], [s, s], Hq, 1, d, T, "f16", window=700, sinks=5, seed=Hq + d + 1)
 
 
+@pytest.mark.parametrize("R,Hkv", [(2, 160), (33, 8), (37, 9), (64, 5), (65, 4), (130, 2)])
+def test_more_workgroups_than_cus(B, R, Hkv):
+    """Up to 64 requests are handed out by their lengths: equal ones, empty ones, requests without queries."""
+    rng = np.random.default_rng(R)
+    lens = rng.choice([0, 1, 40, 40, 100, 300], size=R).tolist()
+    s = [min(n, int(rng.integers(0, 3))) for n in lens]
+    s[0], lens[0] = 2, max(lens[0], 2)
+    check_attention(B, lens, s, Hkv, Hkv, 64, 16, "bf16", seed=R)
+    check_attention(B, lens, s, Hkv, Hkv, 64, 16, "f16", window=30, sinks=3, seed=R)
+
+
+@pytest.mark.parametrize("R,Hkv", [(5, 12), (64, 1), (66, 1)])
+def test_chunks_of_more_workgroups_than_cus(B, R, Hkv):
+    rng = np.random.default_rng(R)
+    lens = rng.choice([30, 90, 90, 161], size=R).tolist()
+    s = [min(n, int(rng.integers(20, 80))) for n in lens]
+    check_attention(B, lens, s, 12 * Hkv, Hkv, 64, 16, "bf16", hints=(1000, 200), seed=R)
+
+
 def test_hints_that_are_too_small_or_missing_change_no_result(B):
     lens, s = [700, 20, 3001], [40, 9, 3]
     for hints in ((0, 0), (1, 1), (1, 3001), (40, 16), (0, 1), (2, 0), (1 << 30, 1 << 30)):
