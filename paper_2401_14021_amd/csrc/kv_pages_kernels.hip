@@ -193,23 +193,26 @@ __global__ __launch_bounds__(256) void take_kernel(KvPages kv, const int32_t *gr
     if (lane == 0) kv.lens[r] = (int32_t)(len + grow[r]);
 }
 
-// The same by one workgroup: a request per thread, neighbouring pages per thread.  16384 pages and 256 requests of which 128 grow: 16 us for the three launches
-// above and their two gaps of 1.5 us, 14.5 us (loads that follow from each other: lengths, last pages, their counts, the list, the table).
+// The same by one workgroup of 1024 threads: a request per thread, and 64 neighbouring pages, whose free ones a wave's vote makes a word of.  What bounds it are loads
+// that follow from each other: lengths, last pages, their counts, the list, the table.
 constexpr int SMALL_PAGES = 65536, SMALL_REQUESTS = 1024;
-// which of the pages base .. base + per - 1 (per <= 64) are free, sixteen counts' loads under way at once; `between` is done while the first of them are
+// words[i]: which of the pages 64 i .. 64 i + 63 are free (as far as there are pages); sixteen counts' loads under way at once, `between` is done while the first of them
+// are.  A barrier follows
 template <class F>
-__device__ __forceinline__ uint64_t free_pages(const KvPages &kv, int base, int per, F between)
+__device__ __forceinline__ void free_words(const KvPages &kv, u64 *words, F between)
 {
-    uint64_t bits = 0;
-    for (int i0 = 0; i0 < per; i0 += 16) {
+    const int tid = threadIdx.x;
+    for (int at = 0; at < kv.n_pages; at += 16384) {
         int c[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) c[i] = i0 + i < per && base + i0 + i < kv.n_pages ? kv.refs[base + i0 + i] : 1;
-        if (i0 == 0) between();
+        for (int i = 0; i < 16; ++i) c[i] = at + i * 1024 + tid < kv.n_pages ? kv.refs[at + i * 1024 + tid] : 1;
+        if (at == 0) between();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bits |= (uint64_t)(c[i] <= 0) << (i0 + i);
+        for (int i = 0; i < 16; ++i) {
+            const u64 bits = __ballot(c[i] <= 0);
+            if ((tid & 63) == 0) words[(at + i * 1024 + tid) >> 6] = bits;
+        }
     }
-    return bits;
 }
 // the sums of v's two halves over the threads in front of this one, and over all 1024
 __device__ __forceinline__ u64 pair_before(u64 v, u64 *red, u64 &total)
@@ -233,20 +236,19 @@ __device__ __forceinline__ u64 pair_before(u64 v, u64 *red, u64 &total)
 }
 __global__ __launch_bounds__(1024) void reserve_small_kernel(KvPages kv, const int32_t *grow, int32_t *granted, int32_t *scratch)
 {
-    __shared__ u64 red[16];
-    __shared__ int s_first[SMALL_REQUESTS], s_place[SMALL_REQUESTS], n_pairs, s_taken;
+    __shared__ u64 red[16], words[SMALL_PAGES / 64];
+    __shared__ int prefix[SMALL_PAGES / 64], s_first[SMALL_REQUESTS], s_place[SMALL_REQUESTS], n_pairs, s_taken;
     const Scratch s = carve(scratch, kv.n_pages, kv.R);
     const int r = threadIdx.x;
     if (r == 0) n_pairs = s_taken = 0;
     int word = 0;
-    const int per = (kv.n_pages + 1023) / 1024, base = r * per;
-    uint64_t bits = free_pages(kv, base, per, [&] { word = r < kv.R ? need_of(kv, grow, r) : 0; });
+    free_words(kv, words, [&] { word = r < kv.R ? need_of(kv, grow, r) : 0; });
+    __syncthreads();
     const int need = word < 0 ? 0 : word & ~NEED_COPY;
     u64 total;
-    const u64 before = pair_before((u64)__popcll(bits) << 32 | (uint32_t)need, red, total);
+    const u64 before = pair_before((u64)(r * 64 < kv.n_pages ? __popcll(words[r]) : 0) << 32 | (uint32_t)need, red, total);
     const int n_free = (int)(total >> 32), wanted = (int)(uint32_t)total, first = (int)(uint32_t)before;
-    int rank = (int)(before >> 32);
-    for (; bits && rank < wanted; bits &= bits - 1, ++rank) s.list[rank] = base + __builtin_ctzll(bits);
+    prefix[r] = (int)(before >> 32);
     const bool ok = word >= 0 && (need == 0 || first + need <= n_free);
     if (ok && need) atomicMax(&s_taken, first + need);   // requests that are served come first, but for those that need nothing
     const bool copy = word >= 0 && (word & NEED_COPY);
@@ -255,6 +257,12 @@ __global__ __launch_bounds__(1024) void reserve_small_kernel(KvPages kv, const i
     if (r < kv.R) len = clamped_len(kv.lens[r], (int64_t)kv.max_pages * T);
     s_first[r] = first;
     s_place[r] = (int)((len + T - 1) / T) * 2 - (copy ? 1 : 0);   // place behind the last page; odd: the page in front of it is copied
+    __syncthreads();
+    for (int id = r; id < kv.n_pages && prefix[(id - r) >> 6] < wanted; id += 1024) {
+        const u64 bits = words[id >> 6];
+        const int rank = prefix[id >> 6] + __popcll(bits & ((1ull << (id & 63)) - 1ull));
+        if ((bits >> (id & 63) & 1u) && rank < wanted) s.list[rank] = id;
+    }
     __syncthreads();
     const int taken = s_taken;
     for (int i = threadIdx.x; i < taken; i += 1024) {
@@ -399,22 +407,26 @@ __global__ __launch_bounds__(256) void movers_kernel(KvPages kv, int32_t *scratc
 // the same by one workgroup, without count_kernel
 __global__ __launch_bounds__(1024) void movers_small_kernel(KvPages kv, int32_t *scratch, int32_t *used_out)
 {
-    __shared__ int red[16];
+    __shared__ int red[16], prefix[SMALL_PAGES / 64];
+    __shared__ u64 words[SMALL_PAGES / 64];
     const Scratch s = carve(scratch, kv.n_pages, kv.R);
-    const int per = (kv.n_pages + 1023) / 1024, base = threadIdx.x * per;
-    const uint64_t bits = free_pages(kv, base, per, [] {});
+    free_words(kv, words, [] {});
+    __syncthreads();
+    const u64 bits = (int)threadIdx.x * 64 < kv.n_pages ? words[threadIdx.x] : 0;
     const int mine = __popcll(bits);
     const int before = sum_before<1024>(mine, red), used = kv.n_pages - group_sum<1024>(mine, red);
-    const int in_front = used <= base ? 0 : used - base >= 64 ? 64 : used - base;   // of this thread's pages, those in front of place `used`
+    prefix[threadIdx.x] = before;
+    const int base = threadIdx.x * 64, in_front = used <= base ? 0 : used - base >= 64 ? 64 : used - base;   // of this thread's pages, those in front of place `used`
     const int holes = group_sum<1024>(__popcll(in_front == 64 ? bits : bits & ((1ull << in_front) - 1ull)), red);
     if (threadIdx.x == 0) {
         s.n_pairs[0] = holes;
         *used_out = used;
     }
     int32_t *place = s.list, *hole = s.list + kv.n_pages, *mover = hole + kv.n_pages;
-    for (int i = 0; i < per && base + i < kv.n_pages; ++i) {
-        const int id = base + i, f = before + __popcll(bits & ((1ull << i) - 1ull));   // free pages in front of id
-        const bool is_free = bits >> i & 1u;
+    for (int id = threadIdx.x; id < kv.n_pages; id += 1024) {
+        const u64 w = words[id >> 6];
+        const int f = prefix[id >> 6] + __popcll(w & ((1ull << (id & 63)) - 1ull));   // free pages in front of id
+        const bool is_free = w >> (id & 63) & 1u;
         if (id < used) {
             if (is_free) hole[f] = id;
         } else if (!is_free) {
