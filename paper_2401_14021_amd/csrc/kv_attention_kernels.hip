@@ -19,6 +19,15 @@
 // Masks: a step of 32 tokens that every row sees takes no test at all.  In the others a token that a row does not see gets the
 // score -inf; its value counts with p = 0, so powers behind the last token (pages that were never written) and of tokens that hold NaN are
 // set aside first (guard_values), as 0 * NaN would reach rows that do not see the token.
+//
+// What bounds it (counters): vector instructions and multiplies, which overlap only in part on a SIMD (a wave of each side by side takes 355 us where alone they take
+// 248 and 245).  Of the 200 vector instructions of a step of 16 rows 96 make operands of codes.  Six contexts of 115000 tokens, 8 x 4 heads of
+// 128: 139 us, 5.5 TB/s of cache, 54 % of the cycles issue vector instructions, 16 % are multiplies; a single token's other limit is the
+// chain offsets -> pages -> codes -> sums (8 us for 640 tokens).  Prompt chunks: 415 us for 274 GFLOP, 660 TFLOP/s; 73 % and 33 %.
+// Tried there and slower: operands converted once per workgroup and passed on through LDS (442 us: a fifth fewer instructions, but the waves wait for each other
+// and for LDS), 48 or 64 rows a wave with the queries in LDS (476 to 490 us), one set of registers for a step's codes to have four waves a
+// SIMD (156 instead of 141 us for the long contexts), loads two and three steps ahead (162 to 165).  fp4 codes as operands of the block-scaled multiply, with the
+// query as two fp8 numbers, need no conversion of the keys, but its sums were found to be good to 1e-4 of the products' magnitude only.
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "kv_kernels.h"
