@@ -126,6 +126,7 @@ ralm_status plan_of(const ralm_kv_t *kv, int32_t n_q_heads, int64_t Qt, int64_t 
     if (n_q_heads < kv->n_heads || n_q_heads % kv->n_heads || n_q_heads > 4096)
         return set_error(RALM_ERR_SHAPE, "n_q_heads=%d must be a multiple of n_heads=%d of at most 4096", n_q_heads, kv->n_heads);
     if (Qt < 0 || Qt > MAX_TOKENS) return set_error(RALM_ERR_RANGE, "Qt=%lld out of [0, 2^22]", (long long)Qt);
+    if (Qt * n_q_heads > (1 << 30)) return set_error(RALM_ERR_SHAPE, "Qt x n_q_heads beyond 2^30; split the batch");
     if (max_q < 0 || max_len < 0 || window < 0 || sinks < 0) return set_error(RALM_ERR_RANGE, "max_q, max_len, window and sinks must not be negative");
     const int64_t room = (int64_t)kv->max_pages * kv->page_tokens;
     if (max_q == 0 || max_q > Qt) max_q = Qt;

@@ -90,53 +90,75 @@ __device__ __forceinline__ int k_power(int row, int b) { return 16 * D + row * (
 template <int D>
 __device__ __forceinline__ int v_power(int row, int b) { return 16 * D + D / 2 + ((row >> 2) * (D / 32) + b) * 4 + (row & 3); }
 
+// Workgroup b runs on XCD b % 8: an XCD gets neighbouring tokens, so that what they share of a line (values of four tokens lie beside each other)
+// comes together in its L2
+__device__ __forceinline__ int64_t unit_of_wave()
+{
+    const uint32_t per = (gridDim.x + 7) / 8, b = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
+    return (int64_t)b * 4 + (threadIdx.x >> 6);
+}
+
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView kv, KvRows rows)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t unit = unit_of_wave();
     const int64_t t = unit >> 1;
     const bool values = unit & 1;
     if (t >= rows.n) return;
     const void *src = values ? rows.v : rows.k;
     const int64_t ts = values ? rows.v_token : rows.k_token, hs = values ? rows.v_head : rows.k_head;
+    constexpr int C = D / 8;   // pieces of a head
+    const int pieces = kv.n_heads * C;
+    // Four steps' loads under way at once, the first of them while the token's place is looked up.  A multiple of four pieces: the lanes of a block come
+    // together
+    float x[4][8];
+    auto load4 = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + 64 * u;
+            if (i < pieces) load8<DT>(src, t * ts + i / C * hs + 8 * (i % C), x[u]);
+        }
+    };
+    load4(lane);
     int row = 0;
     uint8_t *at = place_of(kv, rows, t, row);
     if (!at) return;
-    constexpr int C = D / 8;   // pieces of a head
-    const int pieces = kv.n_heads * C;
-    for (int i = lane; i < pieces; i += 64) {   // a multiple of four pieces: the lanes of a block come together
-        const int h = i / C, c = i % C;
-        float x[8];
-        load8<DT>(src, t * ts + h * hs + 8 * c, x);
-        uint32_t top = 0;   // magnitudes in the order of whole numbers; NaN beyond infinity
+    for (int i0 = lane; i0 < pieces; i0 += 256) {
+        if (i0 != lane) load4(i0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-        top = max(top, lane_xor<1>(top));
-        top = max(top, lane_xor<2>(top));
-        int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u);
-        e = e < 1 ? 1 : e > 252 ? 252 : e;   // 6 * 2^125 at most: 2^128 would be infinite in fp32 (the conversion saturates)
-        const bool odd = top >= 0x7f800000u;
-        const float unit2 = __uint_as_float((uint32_t)e << 23);
-        uint32_t w = 0;
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit2, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit2, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit2, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit2, 3);
-        if (odd) {
-            w = 0;
-            e = 255;
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + 64 * u, h = i / C, c = i % C;
+            if (i >= pieces) break;
+            uint32_t top = 0;   // magnitudes in the order of whole numbers; NaN beyond infinity
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[u][j]) & 0x7fffffffu);
+            top = max(top, lane_xor<1>(top));
+            top = max(top, lane_xor<2>(top));
+            int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u);
+            e = e < 1 ? 1 : e > 252 ? 252 : e;   // 6 * 2^125 at most: 2^128 would be infinite in fp32 (the conversion saturates)
+            const bool odd = top >= 0x7f800000u;
+            const float unit2 = __uint_as_float((uint32_t)e << 23);
+            uint32_t w = 0;
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][0], x[u][1], unit2, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][2], x[u][3], unit2, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][4], x[u][5], unit2, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u][6], x[u][7], unit2, 3);
+            if (odd) {
+                w = 0;
+                e = 255;
+            }
+            uint8_t *tile = at + h * kv.head_bytes;
+            if (!values) {
+                *reinterpret_cast<uint32_t *>(tile + k_codes<D>(row, c)) = w;
+            } else if constexpr (D == 64) {
+                *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c)) = (uint16_t)w;
+                *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c) + D / 8) = (uint16_t)(w >> 16);
+            } else {
+                *reinterpret_cast<uint32_t *>(tile + v_codes<D>(row, c)) = w;
+            }
+            if ((c & 3) == 0) tile[values ? v_power<D>(row, c >> 2) : k_power<D>(row, c >> 2)] = (uint8_t)e;
         }
-        uint8_t *tile = at + h * kv.head_bytes;
-        if (!values) {
-            *reinterpret_cast<uint32_t *>(tile + k_codes<D>(row, c)) = w;
-        } else if constexpr (D == 64) {
-            *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c)) = (uint16_t)w;
-            *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c) + D / 8) = (uint16_t)(w >> 16);
-        } else {
-            *reinterpret_cast<uint32_t *>(tile + v_codes<D>(row, c)) = w;
-        }
-        if ((c & 3) == 0) tile[values ? v_power<D>(row, c >> 2) : k_power<D>(row, c >> 2)] = (uint8_t)e;
     }
 }
 
@@ -144,7 +166,7 @@ template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView kv, KvRows rows)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t unit = unit_of_wave();
     const int64_t t = unit >> 1;
     const bool values = unit & 1;
     if (t >= rows.n) return;
@@ -183,7 +205,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView kv, KvRows rows)
 template <int D>
 hipError_t rows_of(bool append, const KvView &kv, const KvRows &rows, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((rows.n * 2 + 3) / 4));
+    const dim3 grid((unsigned)((rows.n * 2 + 31) / 32 * 8));   // whole rounds of the 8 XCDs
     if (append) {
         if (rows.dtype == DT_F32) kv_append_kernel<D, DT_F32><<<grid, 256, 0, stream>>>(kv, rows);
         else if (rows.dtype == DT_BF16) kv_append_kernel<D, DT_BF16><<<grid, 256, 0, stream>>>(kv, rows);

@@ -79,6 +79,7 @@ def test_attention(b):
     assert at(w=-1) == RANGE and at(f=-1) == RANGE
     assert at(scale=0.0) == RANGE and at(scale=-1.0) == RANGE and at(scale=float("nan")) == RANGE and at(scale=float("inf")) == RANGE
     assert at(heads=6) == SHAPE and at(heads=0) == SHAPE and at(heads=2) == SHAPE and at(heads=8192) == SHAPE
+    assert at(heads=1024, Qt=(1 << 20) + 1, n=1 << 62) == SHAPE             # more than 2^30 rows
     assert at(dt=0) == DTYPE and at(dt=5) == DTYPE
     assert at(q=P + 8) == ALIGN and at(out=P + 4) == ALIGN and at(qs=(1028, 128)) == ALIGN and at(os_=(1024, 100)) == ALIGN
     assert at(ws=None) == WORKSPACE and at(ws=P + 8) == WORKSPACE and at(n=big - 1) == WORKSPACE
