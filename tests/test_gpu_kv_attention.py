@@ -104,6 +104,27 @@ def test_append_values_at_the_edges_of_the_format(B, d):
         np.testing.assert_array_equal(v.double().cpu().numpy(), -want)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_fp16_at_the_edges_of_the_type(B, d):
+    """Subnormal numbers, the largest one, ties at every power, infinities and NaN."""
+    rng = np.random.default_rng(6)
+    n, H = 48, 2
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 4.0, 0.5])
+    x = np.stack([rng.choice(ties, size=(H, d)) * rng.choice([-1, 1], size=(H, d)) * 2.0 ** (t % 30 - 16) for t in range(n)]).astype(np.float16)
+    x[0] = 2.0 ** -24 * rng.integers(-9, 10, size=(H, d))       # subnormal
+    x[1, 0, :32] = 65504.0
+    x[2] = -0.0
+    x[3, 1, 7] = np.inf
+    x[4, 0, d - 1] = np.nan
+    kv = make_cache(B, [n], H, d, 16, seed=8)
+    a = torch.from_numpy(x).cuda()
+    B.ralm_kv_append(kv, 0, a, -a, offsets_of([n]))
+    k, v = B.ralm_kv_read(kv, 0, offsets_of([n]), n, dtype=torch.float32)
+    want = kv_plain.four_bits(x.astype(np.float64))
+    np.testing.assert_array_equal(k.double().cpu().numpy(), want)
+    np.testing.assert_array_equal(v.double().cpu().numpy(), -want)
+
+
 def test_append_writes_its_own_tokens_only(B):
     """A few tokens behind others, from a fused tensor's strided parts; rows of no request and places outside the table are left out."""
     H, d, T, layers = 2, 128, 32, 2
