@@ -28,6 +28,8 @@
 // and for LDS), 48 or 64 rows a wave with the queries in LDS (476 to 490 us), one set of registers for a step's codes to have four waves a
 // SIMD (156 instead of 141 us for the long contexts), loads two and three steps ahead (162 to 165).  fp4 codes as operands of the block-scaled multiply, with the
 // query as two fp8 numbers, need no conversion of the keys, but its sums were found to be good to 1e-4 of the products' magnitude only.
+#include <atomic>
+
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "kv_kernels.h"
@@ -675,15 +677,17 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, 
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <class K>
-hipError_t run(K *kernel, int waves, int lds, const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
+template <auto KERNEL>
+hipError_t run(int waves, int lds, const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream)
 {
     const int64_t groups = ceil_div((int64_t)kv.R * kv.n_heads, 8) * 8 * plan.row_tiles * plan.parts;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static std::atomic<bool> attr_done{false};   // per kernel; setting it twice is harmless
+    if (lds > 65536 && !attr_done.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
+        attr_done.store(true, std::memory_order_release);
     }
-    kernel<<<(unsigned)groups, 64 * waves, lds, stream>>>(kv, a);
+    KERNEL<<<(unsigned)groups, 64 * waves, lds, stream>>>(kv, a);
     return hipGetLastError();
 }
 template <int D, bool HALF>
@@ -698,15 +702,15 @@ hipError_t run_form(const KvView &kv, const KvAttention &a, const KvAttentionPla
         return hipGetLastError();
     };
     constexpr bool EIGHT1 = D <= 128, EIGHT2 = D == 64 || (D == 128 && !HALF);   // eight waves: half the registers a wave
-    if (plan.rows == 64 * N) return finish(run(kv_attention_kernel<D, N, HALF, true, 4>, 4, lds_bytes<D, N, true, 4>(), kv, a, plan, stream));
+    if (plan.rows == 64 * N) return finish(run<kv_attention_kernel<D, N, HALF, true, 4>>(4, lds_bytes<D, N, true, 4>(), kv, a, plan, stream));
     if (plan.waves == 8) {
         if constexpr (EIGHT1)
-            if (plan.rows == 16) return finish(run(kv_attention_kernel<D, 1, HALF, false, 8>, 8, lds_bytes<D, 1, false, 8>(), kv, a, plan, stream));
+            if (plan.rows == 16) return finish(run<kv_attention_kernel<D, 1, HALF, false, 8>>(8, lds_bytes<D, 1, false, 8>(), kv, a, plan, stream));
         if constexpr (EIGHT2)
-            if (plan.rows == 32) return finish(run(kv_attention_kernel<D, 2, HALF, false, 8>, 8, lds_bytes<D, 2, false, 8>(), kv, a, plan, stream));
+            if (plan.rows == 32) return finish(run<kv_attention_kernel<D, 2, HALF, false, 8>>(8, lds_bytes<D, 2, false, 8>(), kv, a, plan, stream));
     }
-    if (plan.rows == 16) return finish(run(kv_attention_kernel<D, 1, HALF, false, 4>, 4, lds_bytes<D, 1, false, 4>(), kv, a, plan, stream));
-    return finish(run(kv_attention_kernel<D, N, HALF, false, 4>, 4, lds_bytes<D, N, false, 4>(), kv, a, plan, stream));
+    if (plan.rows == 16) return finish(run<kv_attention_kernel<D, 1, HALF, false, 4>>(4, lds_bytes<D, 1, false, 4>(), kv, a, plan, stream));
+    return finish(run<kv_attention_kernel<D, N, HALF, false, 4>>(4, lds_bytes<D, N, false, 4>(), kv, a, plan, stream));
 }
 
 }  // namespace
