@@ -720,8 +720,13 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
 {
     KvAttentionPlan p;
     const int64_t rows = (max_q < 1 ? 1 : max_q) * group;
+    // Waves with rows of their own where that gives two workgroups per CU whose waves have nearly all of their rows; else waves that share out the tokens of
+    // 32 rows.  us in a graph, shared out and of their own: 8 chunks of 700 to 1500 tokens 492, 415; 32 requests, 8 x 8 heads x 128, 2000 tokens, 32 of
+    // them new 111, 105; 24 new 91, 103; 16 new 66, 74; 8 x 8 x 4 heads, 3000 tokens, 256 new 148, 141; 128 new 80, 100; one of 512 new 29, 54.
     const int32_t wave_rows = rows <= 16 || d == 256 ? 16 : 32;
-    p.rows = rows <= 2 * wave_rows ? wave_rows : 4 * wave_rows;
+    const int64_t four = ceil_div(rows, 4 * wave_rows);
+    const bool many = R * n_heads * four >= 512 && rows * 10 >= four * 4 * wave_rows * 9;
+    p.rows = many ? 4 * wave_rows : wave_rows;
     p.row_tiles = (int32_t)ceil_div(rows, p.rows);
     p.max_rows = (int32_t)(rows < 0x7fffffff ? rows : 0x7fffffff);
     // tokens that a row tile may see
@@ -734,27 +739,27 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     const int64_t groups = R * n_heads * p.row_tiles;
     // Waves and parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join, and what every part does once.
     // So nothing is split that fills the chip's 256 CUs as it is or is short (80 tiles of 128 numbers).  Where there is at most a workgroup per CU
-    // it has eight waves, and parts make up one per CU; three of four waves each, which is what their registers allow, where parts stay long; with waves
-    // that have rows of their own, two or one.  One workgroup more than that would be a round of its own.
+    // it has eight waves, and parts make up one per CU; three of four waves each, which is what their registers allow, where parts stay long.  One
+    // workgroup more than that would be a round of its own.
     // us in a graph, 4 waves unsplit, 8 waves unsplit, best split: 1 context, 32 heads x 640 tokens 7.9, 7.8, 9.0; x 1280 -, 10.4, 10.2; x 2048 15.0, 13.2,
     // 9.8; 8 x 4 heads x 32768 188, 135, 17.6; 32 requests, 8 x 8 heads, 4 drafts x 2000 26.4, 22.6, 30; 6 x 115000 756, -, 142 (16 parts of 4 waves; 8 of 8
     // waves 148); 64 requests, 8 x 4 heads x 2000 26.8, -, 33.
-    const bool many = p.rows > wave_rows;
     p.waves = 4;
     int64_t parts = 1;
-    if (groups < 256 || (groups == 256 && !many)) {
+    if (groups <= 256) {
         const bool is_short = tiles * d <= 80 * 128;
-        const int64_t one = 256 / groups, two = 512 / groups, three = 768 / groups;
+        const int64_t one = 256 / groups, three = 768 / groups;
         if (three <= MAX_PARTS && tiles >= three * 128) {
             parts = three;
         } else {
-            p.waves = many ? 4 : 8;
-            if (!is_short) parts = many && two <= 16 && tiles >= two * 24 ? two : one;
+            p.waves = 8;
+            if (!is_short) parts = one;
         }
         if (parts > tiles / 16) parts = tiles / 16;   // two steps of each of four waves
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         if (parts < 1) parts = 1;
     }
+    // 64 requests of 200 to 4000 tokens 38.6 -> 32.6 us, of 2000 each 26.6 -> 27.4; chunks of prompts 435 -> 421
     p.by_length = R > 1 && R <= 64 && groups > 256 ? (p.row_tiles == 1 && !many ? 1 : 2) : 0;
     p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);   // a step of every wave
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);

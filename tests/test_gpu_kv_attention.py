@@ -251,6 +251,17 @@ def test_chunks_of_more_workgroups_than_cus(B, R, Hkv):
     check_attention(B, lens, s, 12 * Hkv, Hkv, 64, 16, "bf16", hints=(1000, 200), seed=R)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 50])
+def test_chunks_by_waves_with_rows_of_their_own(B, d, dtype, window):
+    """No hint how many queries a request has: the launch is that of many rows, of which waves have all, some or none."""
+    rng = np.random.default_rng(d + window)
+    lens = [200, 16, 75, 130, 33, 90, 64]
+    s = [min(n, int(rng.integers(20, 76))) for n in lens]
+    check_attention(B, lens, s, 40, 10, d, 32, dtype, window=window, sinks=3, seed=d, hints=(0, 200), nan_at=[(100, "v"), (150, "k"), (190, "v")])
+
+
 def test_hints_that_are_too_small_or_missing_change_no_result(B):
     lens, s = [700, 20, 3001], [40, 9, 3]
     for hints in ((0, 0), (1, 1), (1, 3001), (40, 16), (0, 1), (2, 0), (1 << 30, 1 << 30)):
