@@ -477,6 +477,16 @@ def ralm_kv_page_bytes(n_layers: int, n_heads: int, d: int, page_tokens: int) ->
     return int(n)
 
 
+def _laid_out(t: torch.Tensor) -> torch.Tensor:
+    """An input whose strides the C ABI reads as torch does: 0 is "dense" there, and "repeated" here (``expand``), so a view that repeats
+    is copied."""
+    return t.contiguous() if 0 in t.stride() else t
+
+
+def _repeats(t: torch.Tensor) -> bool:
+    return any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape))
+
+
 def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor):
     ks, vs = k.stride(), v.stride()
     assert k.shape == v.shape and k.shape[1:] == kv._heads and k.dtype == v.dtype and len(ks) == 3 and ks[2] == vs[2] == 1
@@ -486,6 +496,7 @@ def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tenso
 
 def ralm_kv_append(kv: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor) -> None:
     """``k``, ``v`` [n, n_heads, d]: the last tokens of every request (room for them has been reserved)."""
+    k, v = _laid_out(k), _laid_out(v)
     st = _kv_rows(kv, k, v, offsets)
     _check(lib().ralm_kv_append(kv._ref, layer, k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, offsets.data_ptr(), k.shape[0], _stream()))
 
@@ -499,6 +510,7 @@ def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: 
     if v is None:
         v = torch.empty(n, kv.n_heads, kv.d, dtype=k.dtype, device=kv.pages.device)
     st = _kv_rows(kv, k, v, offsets)
+    assert not _repeats(k) and not _repeats(v)
     assert k.shape[0] == n and (start is None or (start.dtype == torch.int32 and start.shape == kv.lens.shape and start.is_contiguous()))
     _check(lib().ralm_kv_read(kv._ref, layer, offsets.data_ptr(), n, _ptr(start), k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, _stream()))
     return k, v
@@ -516,6 +528,7 @@ def ralm_kv_attention(kv: KVCache, layer: int, q: torch.Tensor, offsets: torch.T
                       scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of every request's last tokens (``q`` [Qt, heads, d]) over its cache; ``scale`` None: d ** -0.5."""
+    q = _laid_out(q)
     shape, qs = q.shape, q.stride()
     Qt, heads, d = shape
     assert d == kv.d and qs[2] == 1
@@ -523,7 +536,7 @@ def ralm_kv_attention(kv: KVCache, layer: int, q: torch.Tensor, offsets: torch.T
     if out is None:
         out = torch.empty(shape, dtype=q.dtype, device=q.device)
     os_ = out.stride()
-    assert out.shape == shape and out.dtype == q.dtype and os_[2] == 1
+    assert out.shape == shape and out.dtype == q.dtype and os_[2] == 1 and not (0 in os_ and _repeats(out))
     assert lse is None or (lse.dtype == torch.float32 and lse.shape == shape[:2] and lse.is_contiguous())
     if q.dtype not in _DT:
         raise RalmError(4, f"dtype {q.dtype}")
@@ -594,10 +607,12 @@ def ralm_verify_draft(draft_ids: torch.Tensor, target_probs: torch.Tensor, u: to
     """(accepted drafts [R], next token [R]) int32; ``target_probs`` [Qt + R, V], ``draft_probs`` [Qt, V] or None (certain drafts)."""
     R, Qt = q_offsets.shape[0] - 1, draft_ids.shape[0]
     V = target_probs.shape[1]
+    target_probs = _laid_out(target_probs)
     assert draft_ids.dtype == torch.int32 and u.dtype == torch.float32 and u_next.dtype == torch.float32
     assert q_offsets.dtype == torch.int64 and u.shape == (Qt,) and u_next.shape == (R,) and target_probs.shape[0] == Qt + R
     assert all(t.is_contiguous() for t in (draft_ids, u, u_next, q_offsets)) and target_probs.stride(1) == 1
     if draft_probs is not None:
+        draft_probs = _laid_out(draft_probs)
         assert draft_probs.shape == (Qt, V) and draft_probs.dtype == target_probs.dtype and draft_probs.stride(1) == 1
     dev = target_probs.device
     if workspace is None:
