@@ -596,7 +596,9 @@ __global__ __launch_bounds__(64 * WAVES) void kv_attention_kernel(KvView kv, KvA
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w) {
                     const float mw = sm[w * RW + t * 16 + row];
-                    ll += mw == MINUS_INF ? 0.0f : sl[w * RW + t * 16 + row] * __builtin_amdgcn_exp2f(mw - mm);
+                    const float lw = sl[w * RW + t * 16 + row];
+                    // a wave without a maximum saw nothing (its sum is 0) or keys that are all NaN (its sum is)
+                    ll += mw == MINUS_INF ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);
                 }
                 const float fin = sink.whole ? (ll == 0.0f ? 0.0f : 1.0f / ll) : 1.0f;
                 const int i = at_row / a.group, head = at.h * a.group + at_row - i * a.group;
@@ -645,8 +647,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, 
             float m = stat.x;
 #pragma unroll
             for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
-            const float f = stat.x == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(stat.x - m);   // 0: a part of which the row sees nothing
-            float l = f * stat.y;
+            const float f = stat.x == MINUS_INF ? 0.0f : __builtin_amdgcn_exp2f(stat.x - m);
+            float l = stat.x == MINUS_INF ? stat.y : f * stat.y;   // without a maximum: 0, or NaN
 #pragma unroll
             for (int s = 1; s < 64; s <<= 1) l += __shfl_xor(l, s, 64);
             float y[D / 64] = {};

@@ -385,3 +385,32 @@ def test_on_another_stream_and_replayed_from_a_graph(B):
         B.ralm_kv_append(kv, 0, k, v, off)
         want = B.ralm_kv_attention(kv, 0, q, off, max_q=8, max_len=2500)
         assert torch.equal(got, want), seed
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_nan_keys_that_are_all_a_wave_or_part_sees(B, d, dtype):
+    """3841 tokens are 241 tiles in parts of 24: the newest token is alone in the last one.  Outputs and lse of the rows that see a NaN
+    key are NaN, whoever summed it up."""
+    for s in (1, 3):
+        check_attention(B, [3841], [s], 8, 2, d, 32, dtype, seed=s + d, nan_at=[(3840, "k")])
+    check_attention(B, [3841], [1], 8, 2, d, 32, dtype, seed=d, nan_at=[(t, "k") for t in range(3841)])
+    check_attention(B, [1, 100], [1, 1], 4, 2, d, 32, dtype, seed=d, nan_at=[(0, "k")] + [(1 + t, "k") for t in range(96, 100)])
+
+
+@pytest.mark.parametrize("lens", [[3841], [700, 90]])
+def test_queries_that_are_nan(B, lens):
+    """Their rows are NaN, and no others: those stay within the bounds of their own roundings."""
+    H, d, s = 2, 128, [2] * len(lens)
+    kv = make_cache(B, lens, H, d, 32, seed=1)
+    K, V = fill_cache(B, kv, lens, 0, "f32", 2)
+    q = torch.randn(sum(s), 8, d, generator=torch.Generator().manual_seed(3)).bfloat16()
+    bad = q.clone()
+    bad[0, 3, 7] = float("nan")
+    lse = torch.empty(q.shape[:2], device="cuda")
+    got = B.ralm_kv_attention(kv, 0, bad.cuda(), offsets_of(s), max_q=2, max_len=max(lens), lse=lse).double().cpu().numpy()
+    assert np.isnan(got[0, 3]).all() and np.isnan(got).sum() == d and torch.isnan(lse[0, 3]) and int(torch.isnan(lse).sum()) == 1
+    for r in range(len(lens)):
+        want, _, mag, size = kv_plain.attention(q[2 * r:2 * r + 2].double().numpy(), K[r], V[r], d ** -0.5)
+        off = np.abs(got[2 * r:2 * r + 2] - want) > kv_plain.attention_tolerance("bf16", want, mag, size, d)
+        assert not off.any()                                              # comparisons with NaN are false
