@@ -663,9 +663,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView kv, KvAttention a, 
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (p0 + e) & 63));   // 0 behind the last part
+                    const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (p0 + e) & 63));
+                    // every part has written its sums, zeros for rows that see none of it: NaN values come through a factor of 0
 #pragma unroll
-                    for (int c = 0; c < D / 64; ++c) y[c] += fp == 0.0f || p0 + e >= sp.parts ? 0.0f : fp * v[e][c];   // what a part of factor 0 holds may be anything
+                    for (int c = 0; c < D / 64; ++c) y[c] += p0 + e >= sp.parts ? 0.0f : fp * v[e][c];
                 }
             }
             const float over = l == 0.0f ? 0.0f : 1.0f / l;

@@ -414,3 +414,11 @@ def test_queries_that_are_nan(B, lens):
         want, _, mag, size = kv_plain.attention(q[2 * r:2 * r + 2].double().numpy(), K[r], V[r], d ** -0.5)
         off = np.abs(got[2 * r:2 * r + 2] - want) > kv_plain.attention_tolerance("bf16", want, mag, size, d)
         assert not off.any()                                              # comparisons with NaN are false
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_nan_values_where_a_parts_factor_vanishes(B, d, dtype):
+    """The newest token is alone in the last part, and its scores lie hundreds below the largest: its weight is 0 in fp32, its value NaN."""
+    check_attention(B, [3841], [1], 8, 2, d, 32, dtype, seed=d, scale=10.0, nan_at=[(3840, "v")])
+    check_attention(B, [3841], [3], 8, 2, d, 32, dtype, seed=d, scale=10.0, nan_at=[(3840, "v")])
