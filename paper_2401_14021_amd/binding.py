@@ -504,7 +504,8 @@ def ralm_kv_append(kv: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, of
 def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: Optional[torch.Tensor] = None,
                  dtype: torch.dtype = torch.bfloat16, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None
                  ) -> Tuple[torch.Tensor, torch.Tensor]:
-    """Keys and values [n, n_heads, d] of every request's last tokens, or of those from ``start`` (int32 [R]) on."""
+    """Keys and values [n, n_heads, d] of every request's last tokens, or of those from ``start`` (int32 [R]) on.  Rows
+    of no request are not written: they are what ``k`` and ``v`` held, and undefined where none were given."""
     if k is None:
         k = torch.empty(n, kv.n_heads, kv.d, dtype=dtype, device=kv.pages.device)
     if v is None:

@@ -104,13 +104,15 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&x)[8])
     }
 }
 
-// where a token lies: its tile of head 0 of the layer, and its row in the tile; NULL if it has no place
-__device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &rows, int64_t t, int &row)
+// where a token lies: its tile of head 0 of the layer, and its row in the tile; NULL if it has no place.  owned: whether it is any request's
+__device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &rows, int64_t t, int &row, bool &owned)
 {
+    owned = false;
     const int r = owner_of(rows.offsets, kv.R, t);
     if (r < 0) return nullptr;
     const int64_t o0 = rows.offsets[r], o1 = rows.offsets[r + 1];
     if (t < o0 || t >= o1) return nullptr;
+    owned = true;
     const int64_t at = rows.start ? (int64_t)rows.start[r] + (t - o0) : (int64_t)kv.lens[r] - (o1 - t);
     const int64_t slot = at >> (kv.tile_shift + 4);
     if (at < 0 || slot >= kv.max_pages) return nullptr;
@@ -167,7 +169,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView kv, KvRows rows)
     };
     load4(lane);
     int row = 0;
-    uint8_t *at = place_of(kv, rows, t, row);
+    bool owned;
+    uint8_t *at = place_of(kv, rows, t, row, owned);
     if (!at) return;
     for (int i0 = lane; i0 < pieces; i0 += 256) {
         if (i0 != lane) load4(i0);
@@ -209,7 +212,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView kv, KvRows rows)
     void *dst = values ? rows.v : rows.k;
     const int64_t ts = values ? rows.v_token : rows.k_token, hs = values ? rows.v_head : rows.k_head;
     int row = 0;
-    const uint8_t *at = place_of(kv, rows, t, row);
+    bool owned;
+    const uint8_t *at = place_of(kv, rows, t, row, owned);
+    if (!owned) return;   // the caller's row stays as it is
     constexpr int C = D / 8;
     const int pieces = kv.n_heads * C;
     for (int i = lane; i < pieces; i += 64) {

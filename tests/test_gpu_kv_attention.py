@@ -422,3 +422,21 @@ def test_nan_values_where_a_parts_factor_vanishes(B, d, dtype):
     """The newest token is alone in the last part, and its scores lie hundreds below the largest: its weight is 0 in fp32, its value NaN."""
     check_attention(B, [3841], [1], 8, 2, d, 32, dtype, seed=d, scale=10.0, nan_at=[(3840, "v")])
     check_attention(B, [3841], [3], 8, 2, d, 32, dtype, seed=d, scale=10.0, nan_at=[(3840, "v")])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_read_does_not_write_rows_of_no_request(B, d, dtype):
+    """Into buffers of the caller's: rows in front of the first offset and behind the last stay as they are, tokens without a place become zeros."""
+    lens, H = [20, 0, 33], 3
+    kv = make_cache(B, lens, H, d, 16, seed=d)
+    K, V = fill_cache(B, kv, lens, 0, "f32", seed=d + 1)
+    off = torch.tensor([4, 9, 9, 12], device="cuda")
+    start = torch.tensor([15, 0, 31], dtype=torch.int32, device="cuda")
+    kv.table[2, 2] = -1                                                   # token 32 of the last request has no place
+    k, v = (torch.full((17, H, d), 7.0, device="cuda", dtype=DT[dtype]) for _ in range(2))
+    B.ralm_kv_read(kv, 0, off, 17, start=start, k=k, v=v)
+    for got, held in ((k, K), (v, V)):
+        assert (got[:4] == 7.0).all() and (got[12:] == 7.0).all()
+        want = np.concatenate([held[0][15:], held[2][31:32], np.zeros((2, H, d))])
+        assert np.array_equal(got[4:12].double().cpu().numpy(), torch.from_numpy(want).to(DT[dtype]).double().numpy())
