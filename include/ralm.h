@@ -585,8 +585,8 @@ ralm_status ralm_kv_read(const ralm_kv_t *kv, int32_t layer, const int64_t *offs
  *   q, out     device [Qt, n_q_heads, d], bf16 or fp16; strides in elements
  *              (0: dense), multiples of 8; bases 16-byte aligned
  *   max_q, max_len  the largest s_r and lens[r], as far as the host knows them
- *              (0: Qt, the table's width): they choose the launch.  Smaller than
- *              the truth they cost time, never a result.
+ *              (0: Qt, the table's width): they choose the launch.  Smaller or larger
+ *              than the truth, or missing, they cost time, never a result.
  *   lse        device fp32 [Qt, n_q_heads] or NULL: log sum exp of a row's scores
  *   workspace  ralm_kv_attention_workspace_bytes(), 16-byte aligned (may be NULL
  *              where that is 256): sums of contexts that are split over workgroups
@@ -595,7 +595,7 @@ ralm_status ralm_kv_read(const ralm_kv_t *kv, int32_t layer, const int64_t *offs
  * are fp32; weights are rounded to 8 bits (bf16) or 16 bits (fp16) for their
  * product with V.  A key that is NaN makes the rows that see it NaN, a value the
  * 32 numbers of its block; rows that do not see it are not touched.  Results are
- * the same from call to call.
+ * the same from call to call.  R * n_heads <= 2^23 - 8, Qt * n_q_heads <= 2^30.
  */
 size_t ralm_kv_attention_workspace_bytes(const ralm_kv_t *kv, int32_t n_q_heads, int64_t Qt, int64_t max_q,
                                          int64_t max_len, int32_t window, int32_t sinks);

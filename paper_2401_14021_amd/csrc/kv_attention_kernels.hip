@@ -766,6 +766,9 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     p.by_length = R > 1 && R <= 64 && groups > 256 ? (p.row_tiles == 1 && !many ? 1 : 2) : 0;
     p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);   // a step of every wave
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);
+    // more row tiles than a launch has workgroups for are gone through in turn
+    const int64_t room = KV_MAX_GROUPS / (ceil_div(R * n_heads, 8) * 8 * p.parts);
+    if (p.row_tiles > room) p.row_tiles = (int32_t)room;
     return p;
 }
 

@@ -70,8 +70,11 @@ struct KvAttentionPlan {
     int32_t waves;         // of a workgroup
     int32_t by_length;
     int32_t max_rows;      // of a request and key/value head, as far as the host knows
-    int32_t row_tiles, parts, part_tiles;
+    int32_t row_tiles;     // workgroups that share the row tiles of a request and key/value head and part
+    int32_t parts, part_tiles;
 };
+constexpr int64_t KV_MAX_GROUPS = 1 << 23;                // workgroups of a launch: below 2^32 work-items
+constexpr int64_t KV_MAX_PAIRS = KV_MAX_GROUPS - 8;       // of request and key/value head, whose places are made up to eights
 KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t max_q, int64_t max_len, int32_t window,
                                   int32_t sinks);
 hipError_t launch_kv_attention(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream);

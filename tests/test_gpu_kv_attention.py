@@ -440,3 +440,13 @@ def test_read_does_not_write_rows_of_no_request(B, d, dtype):
         assert (got[:4] == 7.0).all() and (got[12:] == 7.0).all()
         want = np.concatenate([held[0][15:], held[2][31:32], np.zeros((2, H, d))])
         assert np.array_equal(got[4:12].double().cpu().numpy(), torch.from_numpy(want).to(DT[dtype]).double().numpy())
+
+
+def test_many_requests_without_hints(B):
+    """As many row tiles as all queries could make, times all requests, are more workgroups than a launch has: they are gone through in turn."""
+    R = 1 << 14
+    rng = np.random.default_rng(3)
+    lens = rng.integers(1, 4, size=R).tolist()
+    s = [min(n, int(k)) for n, k in zip(lens, rng.integers(0, 3, size=R))]
+    lens[77], s[77] = 90, 70
+    check_attention(B, lens, s, 1, 1, 64, 16, "bf16", hints=(0, 0), seed=5)

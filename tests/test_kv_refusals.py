@@ -120,3 +120,15 @@ def test_drafts(b):
     assert vd(Qt=-1) == RANGE and vd(dt=3) == DTYPE and vd(ts=999) == SHAPE and vd(ds=10) == SHAPE
     assert vd(tp=P + 2) == ALIGN and vd(dp=P + 1, dt=1) == ALIGN
     assert vd(ws=None) == WORKSPACE and vd(ws=P + 8) == WORKSPACE and vd(size=n - 1) == WORKSPACE
+
+
+def test_attention_of_many_requests_without_hints(b):
+    """Any R is served, whatever is known of the queries; only more pairs of request and head than a launch has workgroups are refused."""
+    L = b.lib()
+    for heads in (1, 8, 127):
+        kv = desc(b, R=1 << 16, n_heads=heads, max_pages=64)
+        for max_q in (0, 1, 1 << 16):
+            assert L.ralm_kv_attention_workspace_bytes(kv, heads, 1 << 16, max_q, 0, 0, 0) == 256, (heads, max_q)
+    assert L.ralm_kv_attention_workspace_bytes(desc(b, R=1 << 16, n_heads=128, max_pages=64), 128, 1 << 16, 1, 0, 0, 0) == 0
+    assert L.ralm_kv_attention_workspace_bytes(desc(b, R=(1 << 16) - 1, n_heads=128, max_pages=64), 128, 1 << 16, 0, 0, 0, 0) == 256
+    assert L.ralm_kv_attention_workspace_bytes(desc(b, R=3, n_heads=1), 4096, 1 << 18, 0, 0, 0, 0) == 256
