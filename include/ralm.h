@@ -584,9 +584,11 @@ ralm_status ralm_kv_read(const ralm_kv_t *kv, int32_t layer, const int64_t *offs
  *
  *   q, out     device [Qt, n_q_heads, d], bf16 or fp16; strides in elements
  *              (0: dense), multiples of 8; bases 16-byte aligned
- *   max_q, max_len  the largest s_r and lens[r], as far as the host knows them
- *              (0: Qt, the table's width): they choose the launch.  Smaller or larger
- *              than the truth, or missing, they cost time, never a result.
+ *   max_q, max_len  the largest s_r and lens[r], as far as the host knows them:
+ *              they choose the launch.  0 is unknown, and so is a max_q beyond Qt:
+ *              the launch is then one for the mean Qt / R, and for the table's width.
+ *              Smaller or larger than the truth, or unknown, they cost time, never a
+ *              result.
  *   lse        device fp32 [Qt, n_q_heads] or NULL: log sum exp of a row's scores
  *   workspace  ralm_kv_attention_workspace_bytes(), 16-byte aligned (may be NULL
  *              where that is 256): sums of contexts that are split over workgroups

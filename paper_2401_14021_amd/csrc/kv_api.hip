@@ -129,11 +129,11 @@ ralm_status plan_of(const ralm_kv_t *kv, int32_t n_q_heads, int64_t Qt, int64_t 
     if (Qt * n_q_heads > (1 << 30)) return set_error(RALM_ERR_SHAPE, "Qt x n_q_heads beyond 2^30; split the batch");
     if (max_q < 0 || max_len < 0 || window < 0 || sinks < 0) return set_error(RALM_ERR_RANGE, "max_q, max_len, window and sinks must not be negative");
     const int64_t room = (int64_t)kv->max_pages * kv->page_tokens;
-    if (max_q == 0 || max_q > Qt) max_q = Qt;
+    if (max_q > Qt) max_q = 0;   // says nothing
     if (max_len == 0 || max_len > room) max_len = room;
     if (window > room) window = 0;
     if (kv->R * kv->n_heads > KV_MAX_PAIRS) return set_error(RALM_ERR_SHAPE, "R x n_heads beyond %lld; split the batch", (long long)KV_MAX_PAIRS);
-    plan = kv_attention_plan(kv->R, kv->n_heads, n_q_heads / kv->n_heads, kv->d, max_q, max_len, window, sinks);
+    plan = kv_attention_plan(kv->R, kv->n_heads, n_q_heads / kv->n_heads, kv->d, Qt, max_q, max_len, window, sinks);
     out_bytes = plan.parts > 1 ? (size_t)plan.parts * Qt * n_q_heads * kv->d * 4 : 0;
     bytes = plan.parts > 1 ? out_bytes + (size_t)plan.parts * Qt * n_q_heads * 8 : 256;
     return RALM_OK;

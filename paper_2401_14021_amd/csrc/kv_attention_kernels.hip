@@ -718,11 +718,14 @@ hipError_t run_form(const KvView &kv, const KvAttention &a, const KvAttentionPla
 
 }  // namespace
 
-KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t max_q, int64_t max_len, int32_t window,
-                                  int32_t sinks)
+KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t Qt, int64_t max_q, int64_t max_len,
+                                  int32_t window, int32_t sinks)
 {
     KvAttentionPlan p;
-    const int64_t rows = (max_q < 1 ? 1 : max_q) * group;
+    // Where the most queries of a request are not known, the form is that for their mean: 64 single tokens over 200 to 4000 (8 x 4 heads x 128) take 44 us so,
+    // 32 with the hint and 127 in the form for one request that has them all; one chunk of 512 among them 166, 295 and 221.
+    const int64_t mean_q = max_q > 0 ? max_q : ceil_div(Qt, R);
+    const int64_t rows = (mean_q < 1 ? 1 : mean_q) * group;
     // Waves with rows of their own where that gives two workgroups per CU whose waves have nearly all of their rows; else waves that share out the tokens of
     // 32 rows.  us in a graph, shared out and of their own: 8 chunks of 700 to 1500 tokens 492, 415; 32 requests, 8 x 8 heads x 128, 2000 tokens, 32 of
     // them new 111, 105; 24 new 91, 103; 16 new 66, 74; 8 x 8 x 4 heads, 3000 tokens, 256 new 148, 141; 128 new 80, 100; one of 512 new 29, 54.
@@ -730,8 +733,8 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     const int64_t four = ceil_div(rows, 4 * wave_rows);
     const bool many = R * n_heads * four >= 512 && rows * 10 >= four * 4 * wave_rows * 9;
     p.rows = many ? 4 * wave_rows : wave_rows;
-    p.row_tiles = (int32_t)ceil_div(rows, p.rows);
-    p.max_rows = (int32_t)(rows < 0x7fffffff ? rows : 0x7fffffff);
+    const int64_t row_tiles = ceil_div(rows, p.rows), max_rows = max_q > 0 ? rows : (Qt < 1 ? 1 : Qt) * group;
+    p.max_rows = (int32_t)(max_rows < 0x7fffffff ? max_rows : 0x7fffffff);
     // tokens that a row tile may see
     int64_t seen = max_len < 1 ? 1 : max_len;
     if (window > 0) {
@@ -739,7 +742,7 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
         seen = most < seen ? most : seen;
     }
     const int64_t tiles = ceil_div(seen, KV_TILE);
-    const int64_t groups = R * n_heads * p.row_tiles;
+    const int64_t groups = R * n_heads * row_tiles;
     // Waves and parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join, and what every part does once.
     // So nothing is split that fills the chip's 256 CUs as it is or is short (80 tiles of 128 numbers).  Where there is at most a workgroup per CU
     // it has eight waves, and parts make up one per CU; three of four waves each, which is what their registers allow, where parts stay long.  One
@@ -762,13 +765,22 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
         if (parts > MAX_PARTS) parts = MAX_PARTS;
         if (parts < 1) parts = 1;
     }
-    // 64 requests of 200 to 4000 tokens 38.6 -> 32.6 us, of 2000 each 26.6 -> 27.4; chunks of prompts 435 -> 421
-    p.by_length = R > 1 && R <= 64 && groups > 256 ? (p.row_tiles == 1 && !many ? 1 : 2) : 0;
     p.part_tiles = (int32_t)(ceil_div(ceil_div(tiles, parts), 8) * 8);   // a step of every wave
     p.parts = (int32_t)ceil_div(tiles, p.part_tiles);
-    // more row tiles than a launch has workgroups for are gone through in turn
-    const int64_t room = KV_MAX_GROUPS / (ceil_div(R * n_heads, 8) * 8 * p.parts);
-    if (p.row_tiles > room) p.row_tiles = (int32_t)room;
+    // Row tiles: those of the request with the most rows.  Where only the mean is known, up to twice as many, or 32 workgroups per CU: one that finds no rows costs
+    // 2.5 ns, one too few goes through several row tiles in turn.  An odd number, as those with rows would meet on a part of the CUs otherwise (2 and 4
+    // row tiles of 64 single tokens: 60 and 70 us, 5: 45).  More than a launch has workgroups for are gone through in turn too.
+    const int64_t pairs = ceil_div(R * n_heads, 8) * 8 * p.parts, room = KV_MAX_GROUPS / pairs;
+    int64_t shared = row_tiles;
+    if (max_q <= 0) {
+        const int64_t all = ceil_div(max_rows, p.rows);
+        shared = 2 * row_tiles - 1 > 8192 / pairs ? 2 * row_tiles - 1 : 8192 / pairs;
+        if (shared > all) shared = all;
+        shared -= shared % 2 == 0;
+    }
+    p.row_tiles = (int32_t)(shared < room ? shared : room);
+    // 64 requests of 200 to 4000 tokens 38.6 -> 32.6 us, of 2000 each 26.6 -> 27.4; chunks of prompts 435 -> 421
+    p.by_length = R > 1 && R <= 64 && groups > 256 ? (p.row_tiles == 1 && !many ? 1 : 2) : 0;
     return p;
 }
 

@@ -75,8 +75,9 @@ struct KvAttentionPlan {
 };
 constexpr int64_t KV_MAX_GROUPS = 1 << 23;                // workgroups of a launch: below 2^32 work-items
 constexpr int64_t KV_MAX_PAIRS = KV_MAX_GROUPS - 8;       // of request and key/value head, whose places are made up to eights
-KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t max_q, int64_t max_len, int32_t window,
-                                  int32_t sinks);
+// max_q: most queries of a request, 0 where that is not known
+KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int32_t d, int64_t Qt, int64_t max_q, int64_t max_len,
+                                  int32_t window, int32_t sinks);
 hipError_t launch_kv_attention(const KvView &kv, const KvAttention &a, const KvAttentionPlan &plan, hipStream_t stream);
 
 struct KvPages {

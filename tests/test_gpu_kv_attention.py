@@ -450,3 +450,25 @@ def test_many_requests_without_hints(B):
     s = [min(n, int(k)) for n, k in zip(lens, rng.integers(0, 3, size=R))]
     lens[77], s[77] = 90, 70
     check_attention(B, lens, s, 1, 1, 64, 16, "bf16", hints=(0, 0), seed=5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 50])
+def test_chunks_by_waves_with_rows_of_their_own_by_the_hint(B, d, dtype, window):
+    """A hint of 256 queries in every request: the launch is that of many rows, of which waves have all, some or none."""
+    rng = np.random.default_rng(d + window)
+    lens = [200, 16, 75, 130, 33, 90, 64]
+    s = [min(n, int(rng.integers(50, 76))) for n in lens]
+    assert sum(s) >= 256                                                  # a hint beyond all queries says nothing
+    check_attention(B, lens, s, 40, 10, d, 32, dtype, window=window, sinks=3, seed=d, hints=(256, 200), nan_at=[(100, "v"), (150, "k"), (190, "v")])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_chunk_among_single_tokens_without_a_hint(B, dtype):
+    """The launch is that for the mean: the chunk's row tiles are more than there are workgroups for them."""
+    lens = [1, 300, 17, 33, 90, 2, 64, 150] * 40
+    s = [1] * len(lens)
+    s[1], lens[1] = 290, 300
+    check_attention(B, lens, s, 8, 2, 64, 32, dtype, seed=9, hints=(0, 0))
+    check_attention(B, lens, s, 8, 2, 64, 32, dtype, seed=9, hints=(0, 0), window=40, sinks=2)

@@ -132,3 +132,13 @@ def test_attention_of_many_requests_without_hints(b):
     assert L.ralm_kv_attention_workspace_bytes(desc(b, R=1 << 16, n_heads=128, max_pages=64), 128, 1 << 16, 1, 0, 0, 0) == 0
     assert L.ralm_kv_attention_workspace_bytes(desc(b, R=(1 << 16) - 1, n_heads=128, max_pages=64), 128, 1 << 16, 0, 0, 0, 0) == 256
     assert L.ralm_kv_attention_workspace_bytes(desc(b, R=3, n_heads=1), 4096, 1 << 18, 0, 0, 0, 0) == 256
+
+
+@pytest.mark.parametrize("R,heads,q_heads,d,q", [(32, 8, 32, 128, 1), (16, 4, 16, 64, 2), (20, 4, 16, 256, 5), (6, 8, 32, 128, 1), (1, 8, 8, 128, 9)])
+def test_a_batch_of_equal_requests_is_planned_alike_without_the_hint(b, R, heads, q_heads, d, q):
+    """The workspace says into how many parts contexts are split."""
+    L, kv = b.lib(), desc(b, R=R, n_heads=heads, d=d, max_pages=1 << 12)
+    with_hint = L.ralm_kv_attention_workspace_bytes(kv, q_heads, R * q, q, 60000, 0, 0)
+    assert with_hint > 256
+    for nothing in (0, R * q + 1):
+        assert L.ralm_kv_attention_workspace_bytes(kv, q_heads, R * q, nothing, 60000, 0, 0) == with_hint
