@@ -141,7 +141,8 @@ __device__ __forceinline__ Request request_of(const KvView &kv, const KvAttentio
     return x;
 }
 
-// The request that is the rank-th longest (equal ones in their order), R <= 64, by all lanes of every wave; lds: 64 words, in which the waves write the same.
+// The request that is the rank-th longest (equal ones in their order), R <= 64, by all lanes of every wave; lds: 64 words, in which the waves write the same,
+// and each reads what its own lanes wrote: they are in step, and the fences keep the compiler from moving a read in front of the writes.
 // 64 comparisons of what 16 reads bring: with a read of a lane's register per request this took 2.5 us of a call.
 __device__ __forceinline__ int longest_request(const KvView &kv, int rank, uint32_t *lds)
 {
@@ -150,6 +151,9 @@ __device__ __forceinline__ int longest_request(const KvView &kv, int rank, uint3
     // no two alike; lanes without a request come last.  Beyond 2^25 tokens lengths count as equal
     const uint32_t key = (uint32_t)(len < 0 ? 0 : len > 1 << 25 ? 1 << 25 : len) * 64u + (63u - lane);
     lds[lane] = key;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     uint32_t before = 0;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
