@@ -477,18 +477,12 @@ def ralm_kv_page_bytes(n_layers: int, n_heads: int, d: int, page_tokens: int) ->
     return int(n)
 
 
-def _laid_out(t: torch.Tensor) -> torch.Tensor:
-    """An input whose strides the C ABI reads as torch does: 0 is "dense" there, and "repeated" here (``expand``), so a view that repeats
-    is copied."""
-    return t.contiguous() if 0 in t.stride() else t
-
-
+# A stride of 0 is "dense" in the C ABI and "repeated" here (``expand``): inputs that repeat are copied, outputs refused.
 def _repeats(t: torch.Tensor) -> bool:
     return any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape))
 
 
-def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor):
-    ks, vs = k.stride(), v.stride()
+def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, ks: tuple, vs: tuple, offsets: torch.Tensor):
     assert k.shape == v.shape and k.shape[1:] == kv._heads and k.dtype == v.dtype and len(ks) == 3 and ks[2] == vs[2] == 1
     assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape == kv._offsets
     return ks[0], ks[1], vs[0], vs[1]
@@ -496,8 +490,11 @@ def _kv_rows(kv: KVCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tenso
 
 def ralm_kv_append(kv: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor) -> None:
     """``k``, ``v`` [n, n_heads, d]: the last tokens of every request (room for them has been reserved)."""
-    k, v = _laid_out(k), _laid_out(v)
-    st = _kv_rows(kv, k, v, offsets)
+    ks, vs = k.stride(), v.stride()
+    if 0 in ks or 0 in vs:
+        k, v = k.contiguous(), v.contiguous()
+        ks, vs = k.stride(), v.stride()
+    st = _kv_rows(kv, k, v, ks, vs, offsets)
     _check(lib().ralm_kv_append(kv._ref, layer, k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, offsets.data_ptr(), k.shape[0], _stream()))
 
 
@@ -510,8 +507,8 @@ def ralm_kv_read(kv: KVCache, layer: int, offsets: torch.Tensor, n: int, start: 
         k = torch.empty(n, kv.n_heads, kv.d, dtype=dtype, device=kv.pages.device)
     if v is None:
         v = torch.empty(n, kv.n_heads, kv.d, dtype=k.dtype, device=kv.pages.device)
-    st = _kv_rows(kv, k, v, offsets)
-    assert not _repeats(k) and not _repeats(v)
+    st = _kv_rows(kv, k, v, k.stride(), v.stride(), offsets)
+    assert 0 not in st or not (_repeats(k) or _repeats(v))
     assert k.shape[0] == n and (start is None or (start.dtype == torch.int32 and start.shape == kv.lens.shape and start.is_contiguous()))
     _check(lib().ralm_kv_read(kv._ref, layer, offsets.data_ptr(), n, _ptr(start), k.data_ptr(), v.data_ptr(), _DT[k.dtype], *st, _stream()))
     return k, v
@@ -529,8 +526,10 @@ def ralm_kv_attention(kv: KVCache, layer: int, q: torch.Tensor, offsets: torch.T
                       scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of every request's last tokens (``q`` [Qt, heads, d]) over its cache; ``scale`` None: d ** -0.5."""
-    q = _laid_out(q)
     shape, qs = q.shape, q.stride()
+    if 0 in qs:
+        q = q.contiguous()
+        qs = q.stride()
     Qt, heads, d = shape
     assert d == kv.d and qs[2] == 1
     assert offsets.dtype == torch.int64 and offsets.is_contiguous() and offsets.shape == kv._offsets
@@ -608,20 +607,27 @@ def ralm_verify_draft(draft_ids: torch.Tensor, target_probs: torch.Tensor, u: to
     """(accepted drafts [R], next token [R]) int32; ``target_probs`` [Qt + R, V], ``draft_probs`` [Qt, V] or None (certain drafts)."""
     R, Qt = q_offsets.shape[0] - 1, draft_ids.shape[0]
     V = target_probs.shape[1]
-    target_probs = _laid_out(target_probs)
+    ts = target_probs.stride()
+    if 0 in ts:
+        target_probs = target_probs.contiguous()
+        ts = target_probs.stride()
     assert draft_ids.dtype == torch.int32 and u.dtype == torch.float32 and u_next.dtype == torch.float32
     assert q_offsets.dtype == torch.int64 and u.shape == (Qt,) and u_next.shape == (R,) and target_probs.shape[0] == Qt + R
-    assert all(t.is_contiguous() for t in (draft_ids, u, u_next, q_offsets)) and target_probs.stride(1) == 1
+    assert all(t.is_contiguous() for t in (draft_ids, u, u_next, q_offsets)) and ts[1] == 1
+    ds = (0, 1)
     if draft_probs is not None:
-        draft_probs = _laid_out(draft_probs)
-        assert draft_probs.shape == (Qt, V) and draft_probs.dtype == target_probs.dtype and draft_probs.stride(1) == 1
+        ds = draft_probs.stride()
+        if 0 in ds:
+            draft_probs = draft_probs.contiguous()
+            ds = draft_probs.stride()
+        assert draft_probs.shape == (Qt, V) and draft_probs.dtype == target_probs.dtype and ds[1] == 1
     dev = target_probs.device
     if workspace is None:
         workspace = torch.empty(max(1, int(lib().ralm_verify_draft_workspace_bytes(R, V))), dtype=torch.uint8, device=dev)
     accepted = torch.empty(R, dtype=torch.int32, device=dev)
     token = torch.empty(R, dtype=torch.int32, device=dev)
-    _check(lib().ralm_verify_draft(draft_ids.data_ptr(), _ptr(draft_probs), 0 if draft_probs is None else draft_probs.stride(0),
-                                   target_probs.data_ptr(), target_probs.stride(0), _DT[target_probs.dtype], V, u.data_ptr(),
+    _check(lib().ralm_verify_draft(draft_ids.data_ptr(), _ptr(draft_probs), ds[0],
+                                   target_probs.data_ptr(), ts[0], _DT[target_probs.dtype], V, u.data_ptr(),
                                    u_next.data_ptr(), Qt, q_offsets.data_ptr(), R, accepted.data_ptr(), token.data_ptr(),
                                    workspace.data_ptr(), workspace.numel(), _stream()))
     return accepted, token
