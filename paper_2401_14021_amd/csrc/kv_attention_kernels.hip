@@ -12,7 +12,8 @@
 // lanes of a row, and only when it grows by more than 2^8 (p then stays below 2^8).
 //
 // 4-bit codes become bf16 in one instruction for two (v_cvt_scalef32_pk_bf16_fp4, which applies the power); bf16 holds them exactly and has
-// fp32's range.  p is rounded to bf16 for its product with V (at most 2^-8 of it, as the rounding of a bf16 output); fp16
+// fp32's range.  p is rounded to bf16 for its product with V (at most 2^-8 of it, as the rounding of a bf16 output: 0.0023 of the outputs' size from 64 bits
+// where the output's rounding alone is 0.0017); with 16 bits of p chunks of prompts took 18 % more, windows 14 %, single tokens 2 to 5 %.  fp16
 // queries, and p for them, are split into two bf16 numbers whose products are added: nothing of the query is lost and p keeps 16 bits.
 // Scores, m, l and out are fp32.
 //
@@ -21,9 +22,9 @@
 // set aside first (guard_values), as 0 * NaN would reach rows that do not see the token.
 //
 // What bounds it (counters): vector instructions and multiplies, which overlap only in part on a SIMD (a wave of each side by side takes 355 us where alone they take
-// 248 and 245).  Of the 200 vector instructions of a step of 16 rows 96 make operands of codes.  Six contexts of 115000 tokens, 8 x 4 heads of
-// 128: 139 us, 5.5 TB/s of cache, 54 % of the cycles issue vector instructions, 16 % are multiplies; a single token's other limit is the
-// chain offsets -> pages -> codes -> sums (8 us for 640 tokens).  Prompt chunks: 415 us for 274 GFLOP, 660 TFLOP/s; 73 % and 33 %.
+// 248 and 245).  A step of 16 rows (bf16, 128 numbers) is 290 instructions: 200 vector ones, 96 of which make operands of codes and 16 are multiplies, 8 loads, the rest scalar.
+// Six contexts of 115000 tokens, 8 x 4 heads of 128: 141 us, 5.5 TB/s of cache, vector instructions issue in 54 % of the cycles, the multiplies are busy in 16 %; a
+// single token's other limit is the chain offsets -> pages -> codes -> sums (8 us for 640 tokens).  Prompt chunks: 395 us for 274 GFLOP, 690 TFLOP/s; 74 % and 31 %.
 // Tried there and slower: operands converted once per workgroup and passed on through LDS (442 us: a fifth fewer instructions, but the waves wait for each other
 // and for LDS), 48 or 64 rows a wave with the queries in LDS (476 to 490 us), one set of registers for a step's codes to have four waves a
 // SIMD (156 instead of 141 us for the long contexts), loads two and three steps ahead (162 to 165).  fp4 codes as operands of the block-scaled multiply, with the
@@ -529,7 +530,7 @@ __global__ __launch_bounds__(64 * WAVES) void kv_attention_kernel(KvView kv, KvA
         };
 
         // Two steps a turn with registers of their own, so that none is moved; the loads of the step behind a step are under way during it.  More of them
-        // gain nothing: a wave that is alone on its SIMD takes 0.63 us a step, which are its instructions in a row (290 of about 5 cycles).
+        // gain nothing: a wave that is alone on its SIMD takes 0.63 us a step, which are its 290 instructions in a row, about 5 cycles each.
         Piece<D> xa[2], xb[2];
         uint32_t fa = 0, fb = 0;
         auto request = [&](int k, Piece<D> (&to)[2], uint32_t &f) {
@@ -749,8 +750,11 @@ KvAttentionPlan kv_attention_plan(int64_t R, int32_t n_heads, int32_t group, int
     const int64_t groups = R * n_heads * row_tiles;
     // Waves and parts.  A wave takes 0.63 us for a step of 32 tokens however few waves there are, and a split costs 5 us: the join, and what every part does once.
     // So nothing is split that fills the chip's 256 CUs as it is or is short (80 tiles of 128 numbers).  Where there is at most a workgroup per CU
-    // it has eight waves, and parts make up one per CU; three of four waves each, which is what their registers allow, where parts stay long.  One
-    // workgroup more than that would be a round of its own.
+    // it has eight waves, and parts make up one per CU; three of four waves each where parts stay long.  One workgroup more than are resident would be a round of its own.
+    // All of this is measured with, and true of, 16 rows of 128 bf16 numbers, whose 166 registers let three waves on a SIMD; the plan knows no other form.  Those of 64
+    // numbers hold two to four waves (125 to 191 registers); of 128 numbers two with 32 rows of bf16 (231 to 253) or 16 rows of fp16 (186 to 194), one with 32 rows of
+    // fp16 (265 to 268); of 256 numbers two in bf16 (243 to 253), one in fp16 (271 to 277): there three workgroups a CU are two or three rounds, and where the kernel has no
+    // form of eight waves (256 numbers; 32 rows of 128 fp16 numbers) four do the work of the eight.
     // us in a graph, 4 waves unsplit, 8 waves unsplit, best split: 1 context, 32 heads x 640 tokens 7.9, 7.8, 9.0; x 1280 -, 10.4, 10.2; x 2048 15.0, 13.2,
     // 9.8; 8 x 4 heads x 32768 188, 135, 17.6; 32 requests, 8 x 8 heads, 4 drafts x 2000 26.4, 22.6, 30; 6 x 115000 756, -, 142 (16 parts of 4 waves; 8 of 8
     // waves 148); 64 requests, 8 x 4 heads x 2000 26.8, -, 33.
