@@ -20,7 +20,10 @@
  * shares: a paged cache of keys and values in 4 bits, attention over it, the
  * forking, rolling back and compacting of its pages (ralm_kv_*), and the
  * verification of drafted tokens against a target's probabilities
- * (ralm_verify_draft).
+ * (ralm_verify_draft).  Around that attention: products with their epilogues
+ * (ralm_linear), norms of the residual stream (ralm_residual_norm), rotary
+ * positions on the way into the cache (ralm_kv_append_rotary), and the mixture
+ * of the model's and the neighbours' distributions (ralm_knnlm_target).
  *
  * General conventions
  *   - Unless a parameter says "host", every data pointer is a DEVICE pointer
@@ -676,6 +679,148 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
                               const float *u, const float *u_next, int64_t Qt, const int64_t *q_offsets,
                               int64_t R, int32_t *accepted, int32_t *next_token, void *workspace,
                               size_t workspace_bytes, void *stream);
+
+/*
+ * The rest of the generator's decoder: the products, norms and positions around
+ * its attention, and the distribution that its drafts are verified against.
+ *
+ * ralm_linear  rows times weights, and what usually follows at once:
+ *
+ *     out[i, n] = residual[i, n] + act(x[i] . w[n] + bias[n])                                            gated = 0
+ *     out[i, n] = residual[i, n] + act(x[i] . w[n] + bias[n]) * (x[i] . w[N + n] + bias[N + n])          gated = 1
+ *
+ *   x          device [T, K] of dtype (bf16 or fp16), rows x_stride elements apart
+ *   w          device [N, K] of dtype ([2N, K] if gated), rows w_stride apart
+ *   bias       device [N] ([2N]) of dtype, or NULL
+ *   act        RALM_ACT_*; gelu is x Phi(x), gelu_tanh its usual approximation,
+ *              silu x / (1 + exp(-x))
+ *   residual   device [T, N] of out_dtype, or NULL; it may be out itself (same
+ *              stride), and must not overlap it otherwise
+ *   out        device [T, N] of out_dtype (dtype or fp32); must not overlap x, w or bias
+ *   workspace  ralm_linear_workspace_bytes(), 16-byte aligned (may be NULL where
+ *              that is 0): sums of products that are split over workgroups
+ *
+ * Strides of 0 are dense.  K is a multiple of 8 in [8, 2^17]; x and w are 16-byte
+ * aligned and their strides multiples of 8 elements, at most 2^22; out, residual
+ * and bias are aligned to their type.  T <= 2^22, N <= 2^20 (2^19 gated), T x N <= 2^40.
+ * Products are exact and summed in fp32, everything up to the one rounding to
+ * out_dtype is fp32.  Results are the same from call to call; they may differ in
+ * the last bits with T, which chooses how a sum is split.
+ */
+enum { RALM_ACT_NONE = 0, RALM_ACT_RELU = 1, RALM_ACT_GELU = 2, RALM_ACT_GELU_TANH = 3, RALM_ACT_SILU = 4 };
+size_t ralm_linear_workspace_bytes(int64_t T, int32_t N, int32_t K, int32_t gated);
+ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *w, int64_t w_stride, int32_t N,
+                        int32_t K, int32_t dtype, const void *bias, int32_t act, int32_t gated,
+                        const void *residual, int64_t residual_stride, void *out, int64_t out_stride,
+                        int32_t out_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A block's output into the residual stream, and the stream's norm for the next block:
+ *
+ *     y = x, or norm(x) * post_weight + post_bias with post = 1
+ *     s = residual + scale * gate * y
+ *     out = norm(s) * weight + bias
+ *
+ *   kind RALM_NORM_RMS:    norm(y) = y / sqrt(mean(y^2) + eps)
+ *   kind RALM_NORM_LAYER:  norm(y) = (y - mean(y)) / sqrt(mean((y - mean(y))^2) + eps)
+ *
+ *   x          device [T, D] of x_dtype
+ *   post_weight, post_bias, weight, bias   device [D] of param_dtype; NULL: 1 and 0
+ *   gate       device of x_dtype or NULL (1): [D] with gate_rows = 0, [T, D] with 1
+ *   residual   device [T, D] of sum_dtype or NULL (0)
+ *   sum        device [T, D] of sum_dtype, or NULL (s is not wanted); may be residual
+ *              or x itself (same type and stride)
+ *   out        device [T, D] of out_dtype, or NULL (only s is wanted); may be x
+ *
+ * Apart from that outputs overlap no input and not each other.  Types are fp32, bf16 or fp16, pointers
+ * aligned to them; strides in elements, 0 = dense.  1 <= D <= RALM_MAX_NORM, T <= 2^22.  Statistics and everything
+ * in between are fp32; the norm is taken of s before it is rounded.
+ */
+enum { RALM_NORM_RMS = 0, RALM_NORM_LAYER = 1 };
+#define RALM_MAX_NORM 32768
+typedef struct {
+    int64_t T;
+    int32_t D, kind;
+    float eps, scale;
+    const void *x;
+    int64_t x_stride;
+    int32_t x_dtype, param_dtype;
+    int32_t post;
+    const void *post_weight, *post_bias;
+    const void *gate;
+    int64_t gate_stride;
+    int32_t gate_rows;
+    const void *residual;
+    int64_t residual_stride;
+    void *sum;
+    int64_t sum_stride;
+    int32_t sum_dtype;
+    const void *weight, *bias;
+    void *out;
+    int64_t out_stride;
+    int32_t out_dtype;
+} ralm_norm_t;
+ralm_status ralm_residual_norm(const ralm_norm_t *norm, void *stream);
+
+/*
+ * Rotary positions.  Two numbers a, b of a head that turn together become
+ *
+ *     (a cos t - b sin t) * amplitude,  (b cos t + a sin t) * amplitude,       t = place * freqs[j]
+ *
+ * for the pairs j < rot / 2: the numbers j and j + rot / 2 of the head (interleaved = 0) or
+ * 2 j and 2 j + 1 (interleaved = 1); the numbers from rot on stay.
+ *
+ * ralm_kv_append_rotary  ralm_kv_append with the keys turned on the way in, and
+ *   the queries of the same tokens turned:
+ *   q, q_out   device [n, n_q_heads, d] of dtype; q_out may be q itself (same
+ *              strides) and must overlap no input otherwise.  q NULL: keys and values alone
+ *   k, v, offsets, n, strides   as in ralm_kv_append
+ *   freqs      device fp64 [rot / 2], radians per place; rot even, 0 <= rot <= d
+ *   shift      device int32 [R] or NULL: a token's place is its place in the cache
+ *              (lens[r] - s + i) plus shift[r]
+ *   Angles, turns and their sums are formed in fp64 and rounded to dtype by way of
+ *   fp32, so that a key's codes do not depend on how its turn is formed: the
+ *   cache holds what ralm_kv_append stores of the turned keys.  Queries of no request are not written.
+ *
+ * ralm_rotary_frequencies  (host, no GPU) fp64 frequencies of a plain or scaled base:
+ *   freqs[j] = f_j (m + (1 - m) / factor),  f_j = base^(-2 j / rot),
+ *   m = clamp((context f_j / 2 pi - low) / (high - low), 0, 1): pairs that turn at
+ *   least `high` times within the `context` tokens of the training stay as they are, those that turn
+ *   at most `low` times are slowed down by factor.  context = 0: m = 0 for all.
+ */
+ralm_status ralm_kv_append_rotary(const ralm_kv_t *kv, int32_t layer, const void *q, int64_t q_token_stride,
+                                  int64_t q_head_stride, int32_t n_q_heads, void *q_out, int64_t q_out_token_stride,
+                                  int64_t q_out_head_stride, const void *k, const void *v, int32_t dtype,
+                                  int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                  int64_t v_head_stride, const double *freqs, int32_t rot, int32_t interleaved,
+                                  double amplitude, const int32_t *shift, const int64_t *offsets, int64_t n,
+                                  void *stream);
+ralm_status ralm_rotary_frequencies(double *freqs, int32_t rot, double base, double factor, double context,
+                                    double low, double high);
+
+/*
+ * The target of a verification: the model's distribution mixed with the neighbours'
+ * (Section 5.3; the interpolation of KNN-LM),
+ *
+ *   out[i, v] = (1 - share_i) softmax(logits[i] / temperature)[v] + share_i sum_{j: tokens[i, j] = v} weights[i, j]
+ *
+ *   logits     device [Q, V] of dtype (fp32, bf16, fp16), rows logits_stride elements apart (0: V)
+ *   tokens, weights   device int32, fp32 [Q, k] (of ralm_knnlm_probs); tokens outside
+ *              [0, V) count for nothing.  0 <= k <= RALM_MAX_K
+ *   share      device fp32 [Q] or NULL: share_all for every row
+ *   out        device [Q, V] of out_dtype; may be logits itself (same type and stride)
+ *   workspace  ralm_knnlm_target_workspace_bytes(), 16-byte aligned (may be NULL where that is 0)
+ *
+ * Sums and exponentials are fp32, a token's weights are added in the order of j, one
+ * rounding to out_dtype.  Logits of -inf are probabilities of 0; a row of nothing
+ * else has the neighbours' part alone.  +inf or NaN make their row NaN.  V <= RALM_MAX_VOCABULARY,
+ * Q <= 2^20.
+ */
+size_t ralm_knnlm_target_workspace_bytes(int64_t Q, int32_t V);
+ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t Q, int32_t V, int32_t dtype,
+                              float temperature, const int32_t *tokens, const float *weights, int32_t k,
+                              const float *share, float share_all, void *out, int64_t out_stride,
+                              int32_t out_dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Optimal speculation stride scheduler, OS^3 (Section 4; estimation of its

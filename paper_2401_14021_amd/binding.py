@@ -40,6 +40,17 @@ class ralm_kv_t(ctypes.Structure):
                 ("R", ctypes.c_int64), ("max_pages", ctypes.c_int32)]
 
 
+class ralm_norm_t(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("gate_rows", ctypes.c_int32),
+                ("residual", ctypes.c_void_p), ("residual_stride", ctypes.c_int64),
+                ("sum", ctypes.c_void_p), ("sum_stride", ctypes.c_int64), ("sum_dtype", ctypes.c_int32),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64), ("out_dtype", ctypes.c_int32)]
+
+
 class ralm_counters_t(ctypes.Structure):
     _fields_ = [("unanswered", ctypes.c_int32), ("ladder_overflows", ctypes.c_int32),
                 ("hard_certified", ctypes.c_int32), ("soft_certified", ctypes.c_int32),
@@ -123,8 +134,19 @@ def lib() -> ctypes.CDLL:
         L.ralm_kv_compact.argtypes = [kvp, vp, vp, vp, vp, size, vp]
         L.ralm_verify_draft_workspace_bytes.argtypes = [i64, i32]
         L.ralm_verify_draft.argtypes = [vp, vp, i64, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, size, vp]
+        f32, f64 = ctypes.c_float, ctypes.c_double
+        L.ralm_linear_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        L.ralm_linear.argtypes = [vp, i64, i64, vp, i64, i32, i32, i32, vp, i32, i32, vp, i64, vp, i64, i32, vp, size, vp]
+        L.ralm_residual_norm.argtypes = [ctypes.POINTER(ralm_norm_t), vp]
+        L.ralm_kv_append_rotary.argtypes = [kvp, i32, vp, i64, i64, i32, vp, i64, i64, vp, vp, i32, i64, i64, i64, i64, vp, i32, i32, f64, vp, vp,
+                                            i64, vp]
+        L.ralm_rotary_frequencies.argtypes = [vp, i32, f64, f64, f64, f64, f64]
+        L.ralm_knnlm_target_workspace_bytes.argtypes = [i64, i32]
+        L.ralm_knnlm_target.argtypes = [vp, i64, i64, i32, i32, f32, vp, vp, i32, vp, f32, vp, i64, i32, vp, size, vp]
+        for name in ("ralm_linear", "ralm_residual_norm", "ralm_kv_append_rotary", "ralm_rotary_frequencies", "ralm_knnlm_target"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("ralm_kv_page_bytes", "ralm_kv_attention_workspace_bytes", "ralm_kv_pages_workspace_bytes",
-                     "ralm_verify_draft_workspace_bytes"):
+                     "ralm_verify_draft_workspace_bytes", "ralm_linear_workspace_bytes", "ralm_knnlm_target_workspace_bytes"):
             getattr(L, name).restype = size
         for name in ("ralm_kv_append", "ralm_kv_read", "ralm_kv_attention", "ralm_kv_reserve", "ralm_kv_fork", "ralm_kv_truncate",
                      "ralm_kv_copy_pages", "ralm_kv_compact", "ralm_verify_draft"):
@@ -631,6 +653,204 @@ def ralm_verify_draft(draft_ids: torch.Tensor, target_probs: torch.Tensor, u: to
                                    u_next.data_ptr(), Qt, q_offsets.data_ptr(), R, accepted.data_ptr(), token.data_ptr(),
                                    workspace.data_ptr(), workspace.numel(), _stream()))
     return accepted, token
+
+
+# Tensors of these calls lie on the current device: its stream is the one that the work is put on.
+def _here(*tensors: Optional[torch.Tensor]) -> int:
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise RalmError(8, "a tensor is not on the GPU")
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise RalmError(8, f"a tensor is on GPU {t.get_device()}, the current device is {device}")
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+# The stride between rows of a matrix whose numbers lie side by side (a matrix of one row has no stride).  Inputs that repeat are copied, outputs refused.
+def _matrix(t: torch.Tensor, shape: tuple) -> Tuple[torch.Tensor, int]:
+    assert t.shape == shape, f"shape {tuple(t.shape)}, expected {shape}"
+    a, b = t.stride()
+    if (b != 1 and shape[1] > 1) or (a == 0 and shape[0] > 1):
+        t = t.contiguous()
+        a = t.stride(0)
+    return t, a if shape[0] > 1 else shape[1]
+
+
+def _out_matrix(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, device) -> Tuple[torch.Tensor, int]:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device), shape[1]
+    assert t.shape == shape and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {shape}"
+    a, b = t.stride()
+    assert (b == 1 or shape[1] <= 1) and (a >= shape[1] or shape[0] <= 1), "an output's rows must lie side by side without overlap"
+    return t, a if shape[0] > 1 else shape[1]
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[torch.Tensor]:
+    if t is None:
+        return None
+    assert t.shape == (n,) and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {(n,)}"
+    return t.contiguous()
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def alloc_linear_workspace(T: int, N: int, K: int, gated: bool = False, device="cuda") -> Optional[torch.Tensor]:
+    """For ralm_linear of up to T rows of these sizes; None where none is needed."""
+    n = int(lib().ralm_linear_workspace_bytes(T, N, K, 1 if gated else 0))
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def ralm_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none", gated: bool = False,
+                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``x`` [T, K] times ``w`` [N, K] ([2N, K] gated: gates, then what they multiply), bias, activation, gate, residual: [T, N] of
+    ``out_dtype`` (that of residual or out, or x's)."""
+    T, K = x.shape
+    rows = w.shape[0]
+    N = rows // 2 if gated else rows
+    assert w.dtype == x.dtype and (not gated or rows % 2 == 0)
+    if x.dtype not in _DT:
+        raise RalmError(4, f"dtype {x.dtype}")
+    x, xs = _matrix(x, (T, K))
+    w, ws = _matrix(w, (rows, K))
+    bias = _vector(bias, rows, x.dtype)
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else residual.dtype if residual is not None else x.dtype
+    if out_dtype not in _DT:
+        raise RalmError(4, f"out_dtype {out_dtype}")
+    rs = 0
+    if residual is not None:
+        assert residual.dtype == out_dtype
+        residual, rs = _matrix(residual, (T, N))
+    out, os_ = _out_matrix(out, (T, N), out_dtype, x.device)
+    stream = _here(x, w, bias, residual, out, workspace)
+    if workspace is None:
+        workspace = alloc_linear_workspace(T, N, K, gated, x.device)
+    _check(lib().ralm_linear(x.data_ptr(), xs, T, w.data_ptr(), ws, N, K, _DT[x.dtype], _ptr(bias), ACTIVATIONS[act], 1 if gated else 0,
+                             _ptr(residual), rs, out.data_ptr(), os_, _DT[out_dtype], _ptr(workspace),
+                             0 if workspace is None else workspace.numel(), stream))
+    return out
+
+
+def ralm_residual_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, kind: str = "rms", weight: Optional[torch.Tensor] = None,
+                       bias: Optional[torch.Tensor] = None, post: bool = False, post_weight: Optional[torch.Tensor] = None,
+                       post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-6,
+                       sum: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                       want_sum: bool = True, want_out: bool = True) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(s, norm of s) with s = residual + scale * gate * (x or its norm); s has the type of ``sum``, ``residual`` or ``x``, the norm that of
+    ``out``, ``out_dtype`` or ``x``.  ``weight`` and its like are [D] of one type, ``gate`` [D] or [T, D] of x's."""
+    T, D = x.shape
+    p = ralm_norm_t()
+    p.T, p.D, p.kind, p.eps, p.scale = T, D, {"rms": 0, "layer": 1}[kind], eps, scale
+    params = [t for t in (weight, bias, post_weight, post_bias) if t is not None]
+    pdt = params[0].dtype if params else torch.float32
+    sdt = sum.dtype if sum is not None else residual.dtype if residual is not None else x.dtype
+    odt = out.dtype if out is not None else out_dtype or x.dtype
+    for dt in (x.dtype, pdt, sdt, odt):
+        if dt not in _DT:
+            raise RalmError(4, f"dtype {dt}")
+    assert (want_sum or sum is None) and (want_out or out is None)
+    x, p.x_stride = _matrix(x, (T, D))
+    keep = [_vector(t, D, pdt) for t in (weight, bias, post_weight, post_bias)]
+    p.weight, p.bias, p.post_weight, p.post_bias = (_ptr(t) for t in keep)
+    p.post = 1 if post else 0
+    assert post or (post_weight is None and post_bias is None)
+    if gate is not None:
+        if gate.dim() == 2:
+            assert gate.dtype == x.dtype
+            gate, p.gate_stride = _matrix(gate, (T, D))
+            p.gate_rows = 1
+        else:
+            gate = _vector(gate, D, x.dtype)
+        p.gate = gate.data_ptr()
+    if residual is not None:
+        assert residual.dtype == sdt
+        residual, p.residual_stride = _matrix(residual, (T, D))
+        p.residual = residual.data_ptr()
+    if want_sum:
+        sum, p.sum_stride = _out_matrix(sum, (T, D), sdt, x.device)
+        p.sum = sum.data_ptr()
+    if want_out:
+        out, p.out_stride = _out_matrix(out, (T, D), odt, x.device)
+        p.out = out.data_ptr()
+    p.x, p.x_dtype, p.param_dtype, p.sum_dtype, p.out_dtype = x.data_ptr(), _DT[x.dtype], _DT[pdt], _DT[sdt], _DT[odt]
+    _check(lib().ralm_residual_norm(ctypes.byref(p), _here(x, residual, gate, sum, out, *keep)))
+    return sum, out
+
+
+def ralm_rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, context: float = 0.0, low: float = 1.0,
+                            high: float = 32.0, device="cuda") -> torch.Tensor:
+    """float64 [rot / 2] radians per place, for ralm_kv_append_rotary."""
+    freqs = torch.empty(max(rot, 0) // 2, dtype=torch.float64)
+    _check(lib().ralm_rotary_frequencies(freqs.data_ptr() or None, rot, base, factor, context, low, high))
+    return freqs.to(device)
+
+
+def ralm_kv_append_rotary(kv: KVCache, layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor,
+                          freqs: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0, shift: Optional[torch.Tensor] = None,
+                          q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """ralm_kv_append of the turned keys; the turned queries ``q`` [n, heads, d] (None: keys and values alone).  Rows of no request are not
+    written: they are what ``q_out`` held, and undefined where none was given."""
+    ks, vs = k.stride(), v.stride()
+    if 0 in ks or 0 in vs:
+        k, v = k.contiguous(), v.contiguous()
+        ks, vs = k.stride(), v.stride()
+    st = _kv_rows(kv, k, v, ks, vs, offsets)
+    if k.dtype not in _DT:
+        raise RalmError(4, f"dtype {k.dtype}")
+    assert freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous()
+    assert shift is None or (shift.dtype == torch.int32 and shift.shape == kv.lens.shape and shift.is_contiguous())
+    qs = os_ = (0, 0, 1)
+    heads = 0
+    if q is not None:
+        qs = q.stride()
+        if 0 in qs:
+            q = q.contiguous()
+            qs = q.stride()
+        n, heads, d = q.shape
+        assert n == k.shape[0] and d == kv.d and q.dtype == k.dtype and qs[2] == 1
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        os_ = q_out.stride()
+        assert q_out.shape == q.shape and q_out.dtype == q.dtype and os_[2] == 1 and not (0 in os_ and _repeats(q_out))
+    _check(lib().ralm_kv_append_rotary(kv._ref, layer, _ptr(q), qs[0], qs[1], heads, _ptr(q_out), os_[0], os_[1], k.data_ptr(), v.data_ptr(),
+                                       _DT[k.dtype], *st, freqs.data_ptr() or None, 2 * freqs.shape[0], 1 if interleaved else 0, amplitude,
+                                       _ptr(shift), offsets.data_ptr(), k.shape[0], _here(q, q_out, k, v, freqs, shift, offsets, kv.pages)))
+    return q_out
+
+
+def alloc_knnlm_target_workspace(Q: int, V: int, device="cuda") -> Optional[torch.Tensor]:
+    """For ralm_knnlm_target of up to Q rows; None where none is needed."""
+    n = int(lib().ralm_knnlm_target_workspace_bytes(Q, V))
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def ralm_knnlm_target(logits: torch.Tensor, tokens: torch.Tensor, weights: torch.Tensor, share, temperature: float = 1.0,
+                      out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """(1 - share) softmax(logits / temperature) + share * the neighbours' weights by token: [Q, V].  ``tokens`` int32 and ``weights``
+    fp32 [Q, k] of ralm_knnlm_probs; ``share`` a number or fp32 [Q]."""
+    Q, V = logits.shape
+    k = tokens.shape[1]
+    assert tokens.dtype == torch.int32 and weights.dtype == torch.float32 and tokens.shape == weights.shape == (Q, k)
+    logits, ls = _matrix(logits, (Q, V))
+    if out is not None:
+        out_dtype = out.dtype
+    for dt in (logits.dtype, out_dtype):
+        if dt not in _DT:
+            raise RalmError(4, f"dtype {dt}")
+    out, os_ = _out_matrix(out, (Q, V), out_dtype, logits.device)
+    tokens, weights = tokens.contiguous(), weights.contiguous()
+    rows = _vector(share, Q, torch.float32) if isinstance(share, torch.Tensor) else None
+    stream = _here(logits, tokens, weights, rows, out, workspace)
+    if workspace is None:
+        workspace = alloc_knnlm_target_workspace(Q, V, logits.device)
+    _check(lib().ralm_knnlm_target(logits.data_ptr(), ls, Q, V, _DT[logits.dtype], temperature, tokens.data_ptr(), weights.data_ptr(), k,
+                                   _ptr(rows), 0.0 if rows is not None else float(share), out.data_ptr(), os_, _DT[out_dtype],
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel(), stream))
+    return out
 
 
 def ralm_os3_gamma(strides, matched, gamma_max: float = 0.6) -> float:

@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libralm.so")
 SOURCES = ["ralm_api.hip", "scan_kernels.hip", "scan_held_kernels.hip", "select_kernels.hip", "cache_verify_kernels.hip", "knnlm_kernels.hip",
-           "os3_host.hip", "kv_api.hip", "kv_rows_kernels.hip", "kv_pages_kernels.hip", "kv_attention_kernels.hip", "draft_kernels.hip"]
+           "os3_host.hip", "kv_api.hip", "kv_rows_kernels.hip", "kv_pages_kernels.hip", "kv_attention_kernels.hip", "draft_kernels.hip",
+           "decoder_api.hip", "linear_kernels.hip", "norm_kernels.hip", "target_kernels.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the scan kernel's stage bodies are fully unrolled by design (static register indices)

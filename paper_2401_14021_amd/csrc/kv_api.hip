@@ -5,7 +5,7 @@
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "ralm_kernels.h"
-#include "kv_kernels.h"
+#include "decoder_kernels.h"
 
 using namespace ralm;
 
@@ -166,6 +166,73 @@ ralm_status ralm_kv_read(const ralm_kv_t *kv, int32_t layer, const int64_t *offs
                          int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void *stream)
 {
     return rows(false, kv, layer, k, v, dtype, k_token_stride, k_head_stride, v_token_stride, v_head_stride, offsets, n, start, stream);
+}
+
+ralm_status ralm_kv_append_rotary(const ralm_kv_t *kv, int32_t layer, const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
+                                  void *q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, const void *k, const void *v, int32_t dtype,
+                                  int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const double *freqs,
+                                  int32_t rot, int32_t interleaved, double amplitude, const int32_t *shift, const int64_t *offsets, int64_t n,
+                                  void *stream)
+{
+    int64_t st[4] = {k_token_stride, k_head_stride, v_token_stride, v_head_stride};
+    KV_CHECK(check_rows(kv, layer, k, v, dtype, st, offsets, n));
+    if (rot < 0 || rot > kv->d || (rot & 1)) return set_error(RALM_ERR_SHAPE, "rot=%d must be even and in [0, d = %d]", rot, kv->d);
+    if (interleaved != 0 && interleaved != 1) return set_error(RALM_ERR_RANGE, "interleaved must be 0 or 1");
+    if (!isfinite(amplitude)) return set_error(RALM_ERR_RANGE, "amplitude must be finite");
+    if (q && (n_q_heads < 1 || n_q_heads > 4096)) return set_error(RALM_ERR_SHAPE, "n_q_heads=%d out of [1, 4096]", n_q_heads);
+    if (n == 0) return RALM_OK;
+    if ((q && !q_out) || (rot > 0 && !freqs)) return set_error(RALM_ERR_NULL, "q_out/freqs is NULL");
+    if (!aligned(freqs, 8)) return set_error(RALM_ERR_ALIGN, "freqs must be 8-byte aligned");
+    int64_t qs[4] = {q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride};
+    if (q) {
+        for (int i = 0; i < 4; i += 2) {
+            if (qs[i + 1] == 0) qs[i + 1] = kv->d;
+            if (qs[i] == 0) qs[i] = qs[i + 1] * n_q_heads;
+        }
+        for (int i = 0; i < 4; ++i)
+            if (qs[i] < kv->d || qs[i] * elem_bytes(dtype) % 16)
+                return set_error(RALM_ERR_ALIGN, "strides of q and q_out must be at least d and multiples of 16 bytes");
+        if (!aligned(q, 16) || !aligned(q_out, 16)) return set_error(RALM_ERR_ALIGN, "q and q_out must be 16-byte aligned");
+        if (q == q_out && (qs[0] != qs[2] || qs[1] != qs[3])) return set_error(RALM_ERR_SHAPE, "q_out is q with other strides");
+    }
+    KvRows r;
+    r.k = const_cast<void *>(k);
+    r.v = const_cast<void *>(v);
+    r.dtype = dtype;
+    r.k_token = st[0], r.k_head = st[1], r.v_token = st[2], r.v_head = st[3];
+    r.offsets = offsets;
+    r.n = n;
+    r.start = nullptr;
+    KvRotary t;
+    t.q = q;
+    t.q_out = q_out;
+    t.q_token = qs[0], t.q_head = qs[1], t.o_token = qs[2], t.o_head = qs[3];
+    t.n_q_heads = q ? n_q_heads : 0;
+    t.freqs = freqs;
+    t.half = rot / 2;
+    t.interleaved = interleaved;
+    t.amplitude = amplitude;
+    t.shift = shift;
+    return launched(launch_kv_append_rotary(view_of(kv, layer), r, t, static_cast<hipStream_t>(stream)));
+}
+
+ralm_status ralm_rotary_frequencies(double *freqs, int32_t rot, double base, double factor, double context, double low, double high)
+{
+    if (rot < 0 || (rot & 1)) return set_error(RALM_ERR_SHAPE, "rot=%d must be even and not negative", rot);
+    if (rot > 0 && !freqs) return set_error(RALM_ERR_NULL, "freqs is NULL");
+    if (!(base >= 1.0) || !isfinite(base) || !(factor > 0.0) || !isfinite(factor) || !(context >= 0.0) || !isfinite(context))
+        return set_error(RALM_ERR_RANGE, "base of at least 1, factor above 0 and context of at least 0, all finite");
+    if (context > 0.0 && (!(low >= 0.0) || !(high > low) || !isfinite(high))) return set_error(RALM_ERR_RANGE, "0 <= low < high, both finite");
+    for (int32_t j = 0; j < rot / 2; ++j) {
+        const double f = pow(base, -2.0 * j / rot);
+        double m = 0.0;
+        if (context > 0.0) {
+            m = (context * f / 6.283185307179586476925 - low) / (high - low);
+            m = m < 0.0 ? 0.0 : m > 1.0 ? 1.0 : m;
+        }
+        freqs[j] = f * (m + (1.0 - m) / factor);
+    }
+    return RALM_OK;
 }
 
 size_t ralm_kv_attention_workspace_bytes(const ralm_kv_t *kv, int32_t n_q_heads, int64_t Qt, int64_t max_q, int64_t max_len, int32_t window,

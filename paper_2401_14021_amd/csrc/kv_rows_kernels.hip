@@ -11,7 +11,7 @@
 // lane and step (16 bytes of a 16-bit type), four lanes per block, so that the block's maximum is two exchanges.
 #include "../../include/ralm.h"
 #include "ralm_common.h"
-#include "kv_kernels.h"
+#include "decoder_kernels.h"
 
 namespace ralm {
 
@@ -105,15 +105,16 @@ __device__ __forceinline__ void store8(void *p, int64_t at, const float (&x)[8])
 }
 
 // where a token lies: its tile of head 0 of the layer, and its row in the tile; NULL if it has no place.  owned: whether it is any request's
-__device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &rows, int64_t t, int &row, bool &owned)
+// r, at: its request and place
+__device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &rows, int64_t t, int &row, bool &owned, int &r, int64_t &at)
 {
     owned = false;
-    const int r = owner_of(rows.offsets, kv.R, t);
+    r = owner_of(rows.offsets, kv.R, t);
     if (r < 0) return nullptr;
     const int64_t o0 = rows.offsets[r], o1 = rows.offsets[r + 1];
     if (t < o0 || t >= o1) return nullptr;
     owned = true;
-    const int64_t at = rows.start ? (int64_t)rows.start[r] + (t - o0) : (int64_t)kv.lens[r] - (o1 - t);
+    at = rows.start ? (int64_t)rows.start[r] + (t - o0) : (int64_t)kv.lens[r] - (o1 - t);
     const int64_t slot = at >> (kv.tile_shift + 4);
     if (at < 0 || slot >= kv.max_pages) return nullptr;
     const int32_t page = kv.table[(int64_t)r * kv.max_pages + slot];
@@ -121,6 +122,12 @@ __device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &row
     row = (int)(at & 15);
     const int tile = (int)(at >> 4) & ((1 << kv.tile_shift) - 1);
     return kv.pages + page * kv.page_bytes + kv.layer_bytes + (int64_t)tile * kv_tile_bytes(kv.d);
+}
+__device__ __forceinline__ uint8_t *place_of(const KvView &kv, const KvRows &rows, int64_t t, int &row, bool &owned)
+{
+    int r;
+    int64_t at;
+    return place_of(kv, rows, t, row, owned, r, at);
 }
 
 // byte of a tile where the codes of numbers 8 c .. 8 c + 7 of token `row` begin (D = 64: the second half lies D / 8 bytes on)
@@ -143,6 +150,30 @@ __device__ __forceinline__ int64_t unit_of_wave()
 {
     const uint32_t per = (gridDim.x + 7) / 8, b = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
     return (int64_t)b * 4 + (threadIdx.x >> 6);
+}
+
+// a piece's codes and, by the first lane of the four that share it, their power
+template <int D, int DT>
+__device__ __forceinline__ void store_piece(uint8_t *tile, bool values, int row, int c, const Eight<DT> &x)
+{
+    const uint32_t top = x.top();
+    int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u);
+    e = e < 1 ? 1 : e > 252 ? 252 : e;   // 6 * 2^125 at most: 2^128 would be infinite in fp32 (the conversion saturates)
+    const bool odd = top >= 0x7f800000u;
+    uint32_t w = x.codes(__uint_as_float((uint32_t)e << 23));
+    if (odd) {
+        w = 0;
+        e = 255;
+    }
+    if (!values) {
+        *reinterpret_cast<uint32_t *>(tile + k_codes<D>(row, c)) = w;
+    } else if constexpr (D == 64) {
+        *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c)) = (uint16_t)w;
+        *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c) + D / 8) = (uint16_t)(w >> 16);
+    } else {
+        *reinterpret_cast<uint32_t *>(tile + v_codes<D>(row, c)) = w;
+    }
+    if ((c & 3) == 0) tile[values ? v_power<D>(row, c >> 2) : k_power<D>(row, c >> 2)] = (uint8_t)e;
 }
 
 template <int D, int DT>
@@ -178,25 +209,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView kv, KvRows rows)
         for (int u = 0; u < 4; ++u) {
             const int i = i0 + 64 * u, h = i / C, c = i % C;
             if (i >= pieces) break;
-            const uint32_t top = x[u].top();
-            int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u);
-            e = e < 1 ? 1 : e > 252 ? 252 : e;   // 6 * 2^125 at most: 2^128 would be infinite in fp32 (the conversion saturates)
-            const bool odd = top >= 0x7f800000u;
-            uint32_t w = x[u].codes(__uint_as_float((uint32_t)e << 23));
-            if (odd) {
-                w = 0;
-                e = 255;
-            }
-            uint8_t *tile = at + h * kv.head_bytes;
-            if (!values) {
-                *reinterpret_cast<uint32_t *>(tile + k_codes<D>(row, c)) = w;
-            } else if constexpr (D == 64) {
-                *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c)) = (uint16_t)w;
-                *reinterpret_cast<uint16_t *>(tile + v_codes<D>(row, c) + D / 8) = (uint16_t)(w >> 16);
-            } else {
-                *reinterpret_cast<uint32_t *>(tile + v_codes<D>(row, c)) = w;
-            }
-            if ((c & 3) == 0) tile[values ? v_power<D>(row, c >> 2) : k_power<D>(row, c >> 2)] = (uint8_t)e;
+            store_piece<D>(at + h * kv.head_bytes, values, row, c, x[u]);
         }
     }
 }
@@ -243,6 +256,238 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView kv, KvRows rows)
     }
 }
 
+// ---- rotary positions on the way in ----------------------------------------------------------------
+
+// Numbers as they are and back.  A turned number is a sum in 64 bits that becomes fp32 and then its type: two sides that form the
+// angle alike agree to 2^-50, so that a key's codes do not depend on who formed them.
+template <int DT>
+__device__ __forceinline__ double number(const void *p, int64_t at)
+{
+    if constexpr (DT == DT_F32) return static_cast<const float *>(p)[at];
+    const uint32_t b = static_cast<const uint16_t *>(p)[at];
+    return DT == DT_BF16 ? __uint_as_float(b << 16) : f16_bits_to_f32(b);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t bits_of(double x)
+{
+    float f = (float)x;
+    asm("" : "+v"(f));   // two roundings, as documented: the compiler would make one of them
+    if constexpr (DT == DT_F32) return __float_as_uint(f);
+    else if constexpr (DT == DT_BF16) return __builtin_bit_cast(uint16_t, (__bf16)f);
+    else return __builtin_bit_cast(uint16_t, (_Float16)f);
+}
+template <int DT>
+__device__ __forceinline__ double number_of(const Eight<DT> &x, int j)
+{
+    if constexpr (DT == DT_F32) return __uint_as_float(x.w[j]);
+    const uint32_t b = j & 1 ? x.w[j / 2] >> 16 : x.w[j / 2] & 0xffffu;
+    return DT == DT_BF16 ? __uint_as_float(b << 16) : f16_bits_to_f32(b);
+}
+template <int DT>
+__device__ __forceinline__ void pack(Eight<DT> &x, const double (&y)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (DT == DT_F32) x.w[j] = bits_of<DT>(y[j]);
+        else if (j & 1) x.w[j / 2] |= bits_of<DT>(y[j]) << 16;
+        else x.w[j / 2] = bits_of<DT>(y[j]);
+    }
+}
+template <int DT>
+__device__ __forceinline__ void store_bits(void *p, int64_t at, uint32_t b)
+{
+    if constexpr (DT == DT_F32) static_cast<uint32_t *>(p)[at] = b;
+    else static_cast<uint16_t *>(p)[at] = (uint16_t)b;
+}
+template <int DT>
+__device__ __forceinline__ void store_eight(void *p, int64_t at, const Eight<DT> &x)
+{
+    if constexpr (DT == DT_F32) {
+        uint4 *d = reinterpret_cast<uint4 *>(static_cast<float *>(p) + at);
+        d[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+        d[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    } else {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + at) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    }
+}
+
+// A workgroup takes TOK tokens: their places, the angles' cosines and sines into LDS once for all heads, then queries, keys and values.
+// WHOLE: pairs lie in pieces of 8 that are loaded whole (half a multiple of 8, or of 4 interleaved); otherwise pair by pair.
+template <int D, int DT, int TOK, bool WHOLE>
+__global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows rows, KvRotary p)
+{
+    constexpr int C = D / 8;   // pieces of a head
+    __shared__ double2 turns[TOK][D / 2];
+    __shared__ uint8_t *tile_at[TOK];
+    __shared__ int64_t place[TOK];
+    __shared__ int row_at[TOK], is_owned[TOK];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // tokens beside each other on one XCD, as in the append
+    const uint32_t per = (gridDim.x + 7) / 8, b = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
+    const int64_t t0 = (int64_t)b * TOK;
+    const int half = p.half;
+    if (wave < TOK) {
+        const int64_t t = t0 + wave;
+        int row = 0, r = 0;
+        int64_t at = 0;
+        bool owned = false;
+        uint8_t *tile = t < rows.n ? place_of(kv, rows, t, row, owned, r, at) : nullptr;
+        if (owned && p.shift) at += p.shift[r];
+        if (lane == 0) tile_at[wave] = tile, place[wave] = at, row_at[wave] = row, is_owned[wave] = owned;
+    }
+    __syncthreads();
+    for (int i = tid; i < TOK * half; i += 256) {
+        const int k = i / half, j = i - k * half;
+        double c, s;
+        sincos((double)place[k] * p.freqs[j], &s, &c);
+        turns[k][j] = make_double2(c * p.amplitude, s * p.amplitude);
+    }
+    __syncthreads();
+    for (int k = 0; k < TOK; ++k) {
+        if (!is_owned[k]) continue;
+        const int64_t t = t0 + k;
+        if (p.q) {
+            const int64_t in = t * p.q_token, to = t * p.o_token;
+            if constexpr (WHOLE) {
+                if (p.interleaved) {
+                    for (int i = tid; i < p.n_q_heads * C; i += 256) {
+                        const int h = i / C, c = i % C;
+                        Eight<DT> x;
+                        x.load(p.q, in + h * p.q_head + 8 * c);
+                        if (8 * c < 2 * half) {
+                            double y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; j += 2) {
+                                const double2 cs = turns[k][4 * c + j / 2];
+                                const double u = number_of<DT>(x, j), v = number_of<DT>(x, j + 1);
+                                y[j] = u * cs.x - v * cs.y;
+                                y[j + 1] = v * cs.x + u * cs.y;
+                            }
+                            pack<DT>(x, y);
+                        }
+                        store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c, x);
+                    }
+                } else {
+                    // a piece of the lower half together with its partner in the upper one; pieces that do not turn by themselves
+                    const int low = half / 8, units = C - low;
+                    for (int i = tid; i < p.n_q_heads * units; i += 256) {
+                        const int h = i / units, c = i - h * units;
+                        Eight<DT> x;
+                        if (c < low) {
+                            Eight<DT> z;
+                            x.load(p.q, in + h * p.q_head + 8 * c);
+                            z.load(p.q, in + h * p.q_head + 8 * c + half);
+                            double y[8], w[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const double2 cs = turns[k][8 * c + j];
+                                const double u = number_of<DT>(x, j), v = number_of<DT>(z, j);
+                                y[j] = u * cs.x - v * cs.y;
+                                w[j] = v * cs.x + u * cs.y;
+                            }
+                            pack<DT>(x, y);
+                            pack<DT>(z, w);
+                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c, x);
+                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c + half, z);
+                        } else {
+                            x.load(p.q, in + h * p.q_head + 8 * (c + low));
+                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * (c + low), x);
+                        }
+                    }
+                }
+            } else {
+                // pairs, then what does not turn
+                const int units = D - half;
+                for (int i = tid; i < p.n_q_heads * units; i += 256) {
+                    const int h = i / units, j = i - h * units;
+                    const int64_t a = in + h * p.q_head, o = to + h * p.o_head;
+                    if (j < half) {
+                        const int e0 = p.interleaved ? 2 * j : j, e1 = p.interleaved ? 2 * j + 1 : j + half;
+                        const double2 cs = turns[k][j];
+                        const double u = number<DT>(p.q, a + e0), v = number<DT>(p.q, a + e1);
+                        store_bits<DT>(p.q_out, o + e0, bits_of<DT>(u * cs.x - v * cs.y));
+                        store_bits<DT>(p.q_out, o + e1, bits_of<DT>(v * cs.x + u * cs.y));
+                    } else {
+                        store_bits<DT>(p.q_out, o + j + half, bits_of<DT>(number<DT>(p.q, a + j + half)));
+                    }
+                }
+            }
+        }
+        uint8_t *at = tile_at[k];
+        if (!at) continue;
+        // keys: a lane turns its own piece, for which it reads the partners too; values go in as they are
+        const int row = row_at[k];
+        for (int i = tid; i < 2 * kv.n_heads * C; i += 256) {
+            const bool values = i >= kv.n_heads * C;
+            const int u = values ? i - kv.n_heads * C : i, h = u / C, c = u % C;
+            Eight<DT> x;
+            if (values) {
+                x.load(rows.v, t * rows.v_token + h * rows.v_head + 8 * c);
+            } else {
+                const int64_t in = t * rows.k_token + h * rows.k_head;
+                x.load(rows.k, in + 8 * c);
+                if (8 * c < 2 * half) {
+                    double y[8];
+                    if constexpr (WHOLE) {
+                        if (p.interleaved) {
+#pragma unroll
+                            for (int j = 0; j < 8; j += 2) {
+                                const double2 cs = turns[k][4 * c + j / 2];
+                                const double a = number_of<DT>(x, j), b2 = number_of<DT>(x, j + 1);
+                                y[j] = a * cs.x - b2 * cs.y;
+                                y[j + 1] = b2 * cs.x + a * cs.y;
+                            }
+                        } else {
+                            const bool low = 8 * c < half;
+                            Eight<DT> z;
+                            z.load(rows.k, in + (low ? 8 * c + half : 8 * c - half));
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const double2 cs = turns[k][(low ? 8 * c : 8 * c - half) + j];
+                                const double a = number_of<DT>(x, j), b2 = number_of<DT>(z, j);
+                                y[j] = low ? a * cs.x - b2 * cs.y : a * cs.x + b2 * cs.y;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int e = 8 * c + j;
+                            const double a = number_of<DT>(x, j);
+                            y[j] = a;
+                            if (e < 2 * half) {
+                                const bool low = p.interleaved ? (e & 1) == 0 : e < half;
+                                const int other = p.interleaved ? e ^ 1 : low ? e + half : e - half;
+                                const double2 cs = turns[k][p.interleaved ? e >> 1 : low ? e : e - half];
+                                const double b2 = number<DT>(rows.k, in + other);
+                                y[j] = low ? a * cs.x - b2 * cs.y : a * cs.x + b2 * cs.y;
+                            }
+                        }
+                    }
+                    pack<DT>(x, y);
+                }
+            }
+            store_piece<D>(at + h * kv.head_bytes, values, row, c, x);
+        }
+    }
+}
+
+template <int D, int DT>
+hipError_t rotary_of(const KvView &kv, const KvRows &rows, const KvRotary &p, hipStream_t stream)
+{
+    const bool whole = p.interleaved ? p.half % 4 == 0 : p.half % 8 == 0;
+    const dim3 grid((unsigned)((rows.n + 7) / 8 * 8));
+    if (whole) kv_append_rotary_kernel<D, DT, 1, true><<<grid, 256, 0, stream>>>(kv, rows, p);
+    else kv_append_rotary_kernel<D, DT, 1, false><<<grid, 256, 0, stream>>>(kv, rows, p);
+    return hipGetLastError();
+}
+template <int D>
+hipError_t rotary_any(const KvView &kv, const KvRows &rows, const KvRotary &p, hipStream_t stream)
+{
+    return rows.dtype == DT_F32    ? rotary_of<D, DT_F32>(kv, rows, p, stream)
+           : rows.dtype == DT_BF16 ? rotary_of<D, DT_BF16>(kv, rows, p, stream)
+                                   : rotary_of<D, DT_F16>(kv, rows, p, stream);
+}
+
 template <int D>
 hipError_t rows_of(bool append, const KvView &kv, const KvRows &rows, hipStream_t stream)
 {
@@ -268,5 +513,9 @@ hipError_t any_rows(bool append, const KvView &kv, const KvRows &rows, hipStream
 
 hipError_t launch_kv_append(const KvView &kv, const KvRows &rows, hipStream_t stream) { return any_rows(true, kv, rows, stream); }
 hipError_t launch_kv_read(const KvView &kv, const KvRows &rows, hipStream_t stream) { return any_rows(false, kv, rows, stream); }
+hipError_t launch_kv_append_rotary(const KvView &kv, const KvRows &rows, const KvRotary &p, hipStream_t stream)
+{
+    return kv.d == 64 ? rotary_any<64>(kv, rows, p, stream) : kv.d == 128 ? rotary_any<128>(kv, rows, p, stream) : rotary_any<256>(kv, rows, p, stream);
+}
 
 }  // namespace ralm
