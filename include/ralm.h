@@ -702,7 +702,7 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
  *
  * Strides of 0 are dense.  K is a multiple of 8 in [8, 2^17]; x and w are 16-byte
  * aligned and their strides multiples of 8 elements, at most 2^22; out, residual
- * and bias are aligned to their type.  T <= 2^22, N <= 2^20 (2^19 gated), T x N <= 2^40.
+ * and bias are aligned to their type.  T <= 2^22, N <= 2^20 (2^19 gated), T x N <= 2^36.
  * Products are exact and summed in fp32, everything up to the one rounding to
  * out_dtype is fp32.  Results are the same from call to call; they may differ in
  * the last bits with T, which chooses how a sum is split.

@@ -28,9 +28,10 @@ ralm_status check_linear(int64_t T, int32_t N, int32_t K, int32_t gated)
     if (T < 0 || T > MAX_ROWS) return set_error(RALM_ERR_SHAPE, "T=%lld out of [0, 2^22]", (long long)T);
     if (N < 1 || N > (1 << 20) >> gated) return set_error(RALM_ERR_SHAPE, "N=%d out of [1, 2^20] (2^19 gated)", N);
     if (K < 8 || K > MAX_K_LINEAR || K % 8) return set_error(RALM_ERR_SHAPE, "K=%d must be a multiple of 8 in [8, 2^17]", K);
-    if (T * N > 1LL << 40) return set_error(RALM_ERR_SHAPE, "T x N beyond 2^40; split the rows");
+    if (T * N > 1LL << 36) return set_error(RALM_ERR_SHAPE, "T x N beyond 2^36; split the rows");
     return RALM_OK;
 }
+size_t sums_bytes(const LinearPlan &plan, int64_t T) { return plan.parts > 1 ? (size_t)plan.parts * T * plan.pitch * 4 : 0; }
 
 }  // namespace
 
@@ -38,7 +39,8 @@ extern "C" {
 
 size_t ralm_linear_workspace_bytes(int64_t T, int32_t N, int32_t K, int32_t gated)
 {
-    return check_linear(T, N, K, gated) == RALM_OK ? 0 : 0;
+    if (check_linear(T, N, K, gated) != RALM_OK || T == 0) return 0;
+    return sums_bytes(linear_plan(T, N, K, gated), T);
 }
 
 ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *w, int64_t w_stride, int32_t N, int32_t K, int32_t dtype,
@@ -64,7 +66,12 @@ ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *
     if (!aligned(out, bytes_of(out_dtype)) || !aligned(residual, bytes_of(out_dtype)) || !aligned(bias, 2))
         return set_error(RALM_ERR_ALIGN, "out, residual and bias must be aligned to their type");
     if (residual == out && residual_stride != out_stride) return set_error(RALM_ERR_SHAPE, "residual is out with another stride");
-    (void)workspace, (void)workspace_bytes;
+    LinearPlan plan = linear_plan(T, N, K, gated);
+    if (plan.parts > 1) {
+        if (!workspace || !aligned(workspace, 16)) return set_error(RALM_ERR_WORKSPACE, "workspace is NULL or not 16-byte aligned");
+        if (workspace_bytes < sums_bytes(plan, T)) return set_error(RALM_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, sums_bytes(plan, T));
+        plan.sums = static_cast<float *>(workspace);
+    }
     LinearParams p;
     p.x = x, p.w = w;
     p.x_stride = x_stride, p.w_stride = w_stride;
@@ -77,7 +84,7 @@ ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *
     p.out = out;
     p.out_stride = out_stride;
     p.out_dtype = out_dtype;
-    return launched(launch_linear(p, static_cast<hipStream_t>(stream)));
+    return launched(launch_linear(p, plan, static_cast<hipStream_t>(stream)));
 }
 
 ralm_status ralm_residual_norm(const ralm_norm_t *norm, void *stream)

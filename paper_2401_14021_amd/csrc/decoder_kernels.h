@@ -22,7 +22,16 @@ struct LinearParams {
     int64_t out_stride;
     int32_t out_dtype;
 };
-hipError_t launch_linear(const LinearParams &p, hipStream_t stream);
+// weights x rows of a workgroup
+enum { LINEAR_FEW_16, LINEAR_FEW_32, LINEAR_128x64, LINEAR_128x128, LINEAR_256x192, LINEAR_256x256 };
+struct LinearPlan {
+    int32_t form;
+    int32_t parts, part_strips;   // of the depth: workgroups that share it, strips of 64 each
+    int64_t pitch;                // of the parts' sums, [parts][T][pitch]
+    float *sums;
+};
+LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated);
+hipError_t launch_linear(const LinearParams &p, const LinearPlan &plan, hipStream_t stream);
 
 hipError_t launch_residual_norm(const ralm_norm_t &p, hipStream_t stream);
 

@@ -29,7 +29,7 @@ def test_linear(b):
     assert at(x=None) == NULL and at(w=None) == NULL and at(out=None) == NULL
     assert at(T=-1) == SHAPE and at(T=(1 << 22) + 1) == SHAPE and at(N=0) == SHAPE and at(N=(1 << 20) + 1) == SHAPE
     assert at(N=(1 << 19) + 1, gated=1) == SHAPE and at(K=0) == SHAPE and at(K=12) == SHAPE and at(K=(1 << 17) + 8) == SHAPE
-    assert at(T=1 << 22, N=(1 << 18) + 1) == SHAPE
+    assert at(T=1 << 22, N=(1 << 14) + 1) == SHAPE
     assert at(dt=F32) == DTYPE and at(dt=7) == DTYPE and at(odt=F16) == DTYPE and at(odt=9) == DTYPE
     assert at(act=-1) == RANGE and at(act=5) == RANGE and at(gated=2) == RANGE
     assert at(xs=56) == SHAPE and at(ws=56) == SHAPE and at(os_=127) == SHAPE and at(res=P, rs=100) == SHAPE
