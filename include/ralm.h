@@ -814,7 +814,7 @@ ralm_status ralm_rotary_frequencies(double *freqs, int32_t rot, double base, dou
  * Sums and exponentials are fp32, a token's weights are added in the order of j, one
  * rounding to out_dtype.  Logits of -inf are probabilities of 0; a row of nothing
  * else has the neighbours' part alone.  +inf or NaN make their row NaN.  V <= RALM_MAX_VOCABULARY,
- * Q <= 2^20.
+ * Q <= 2^20, Q x V <= 2^36 (2^20 rows of up to 65536 entries).  Probabilities below 2^-126 may be 0.
  */
 size_t ralm_knnlm_target_workspace_bytes(int64_t Q, int32_t V);
 ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t Q, int32_t V, int32_t dtype,

@@ -656,41 +656,51 @@ def ralm_verify_draft(draft_ids: torch.Tensor, target_probs: torch.Tensor, u: to
 
 
 # Tensors of these calls lie on the current device: its stream is the one that the work is put on.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _here(*tensors: Optional[torch.Tensor]) -> int:
+    on = None
     for t in tensors:
-        if t is not None and not t.is_cuda:
+        if t is None:
+            continue
+        device = t.get_device()   # -1: the host's
+        if device < 0:
             raise RalmError(8, "a tensor is not on the GPU")
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise RalmError(8, f"a tensor is on GPU {t.get_device()}, the current device is {device}")
+        if on is None:
+            on = device
+        elif on != device:
+            raise RalmError(8, f"tensors are on GPU {on} and {device}")
+    device = _current_device()
+    if on != device:
+        raise RalmError(8, f"tensors are on GPU {on}, the current device is {device}")
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 # The stride between rows of a matrix whose numbers lie side by side (a matrix of one row has no stride).  Inputs that repeat are copied, outputs refused.
-def _matrix(t: torch.Tensor, shape: tuple) -> Tuple[torch.Tensor, int]:
-    assert t.shape == shape, f"shape {tuple(t.shape)}, expected {shape}"
+def _matrix(t: torch.Tensor, T: int, n: int) -> Tuple[torch.Tensor, int]:
+    assert t.shape == (T, n), f"shape {tuple(t.shape)}, expected {(T, n)}"
     a, b = t.stride()
-    if (b != 1 and shape[1] > 1) or (a == 0 and shape[0] > 1):
+    if (b != 1 and n > 1) or (a == 0 and T > 1):
         t = t.contiguous()
         a = t.stride(0)
-    return t, a if shape[0] > 1 else shape[1]
+    return t, a if T > 1 else n
 
 
-def _out_matrix(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, device) -> Tuple[torch.Tensor, int]:
+def _out_matrix(t: Optional[torch.Tensor], T: int, n: int, dtype: torch.dtype, device) -> Tuple[torch.Tensor, int]:
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device), shape[1]
-    assert t.shape == shape and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {shape}"
+        return torch.empty((T, n), dtype=dtype, device=device), n
+    assert t.shape == (T, n) and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {(T, n)}"
     a, b = t.stride()
-    assert (b == 1 or shape[1] <= 1) and (a >= shape[1] or shape[0] <= 1), "an output's rows must lie side by side without overlap"
-    return t, a if shape[0] > 1 else shape[1]
+    assert (b == 1 or n <= 1) and (a >= n or T <= 1), "an output's rows must lie side by side without overlap"
+    return t, a if T > 1 else n
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[torch.Tensor]:
     if t is None:
         return None
     assert t.shape == (n,) and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {(n,)}"
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
 
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
@@ -713,8 +723,8 @@ def ralm_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] =
     assert w.dtype == x.dtype and (not gated or rows % 2 == 0)
     if x.dtype not in _DT:
         raise RalmError(4, f"dtype {x.dtype}")
-    x, xs = _matrix(x, (T, K))
-    w, ws = _matrix(w, (rows, K))
+    x, xs = _matrix(x, T, K)
+    w, ws = _matrix(w, rows, K)
     bias = _vector(bias, rows, x.dtype)
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else residual.dtype if residual is not None else x.dtype
@@ -723,8 +733,8 @@ def ralm_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] =
     rs = 0
     if residual is not None:
         assert residual.dtype == out_dtype
-        residual, rs = _matrix(residual, (T, N))
-    out, os_ = _out_matrix(out, (T, N), out_dtype, x.device)
+        residual, rs = _matrix(residual, T, N)
+    out, os_ = _out_matrix(out, T, N, out_dtype, x.device)
     stream = _here(x, w, bias, residual, out, workspace)
     if workspace is None:
         workspace = alloc_linear_workspace(T, N, K, gated, x.device)
@@ -732,6 +742,9 @@ def ralm_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] =
                              _ptr(residual), rs, out.data_ptr(), os_, _DT[out_dtype], _ptr(workspace),
                              0 if workspace is None else workspace.numel(), stream))
     return out
+
+
+_NORMS = {"rms": 0, "layer": 1}
 
 
 def ralm_residual_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, *, kind: str = "rms", weight: Optional[torch.Tensor] = None,
@@ -742,41 +755,38 @@ def ralm_residual_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None,
     """(s, norm of s) with s = residual + scale * gate * (x or its norm); s has the type of ``sum``, ``residual`` or ``x``, the norm that of
     ``out``, ``out_dtype`` or ``x``.  ``weight`` and its like are [D] of one type, ``gate`` [D] or [T, D] of x's."""
     T, D = x.shape
-    p = ralm_norm_t()
-    p.T, p.D, p.kind, p.eps, p.scale = T, D, {"rms": 0, "layer": 1}[kind], eps, scale
-    params = [t for t in (weight, bias, post_weight, post_bias) if t is not None]
-    pdt = params[0].dtype if params else torch.float32
-    sdt = sum.dtype if sum is not None else residual.dtype if residual is not None else x.dtype
-    odt = out.dtype if out is not None else out_dtype or x.dtype
-    for dt in (x.dtype, pdt, sdt, odt):
+    xdt = x.dtype
+    params = weight if weight is not None else bias if bias is not None else post_weight if post_weight is not None else post_bias
+    pdt = torch.float32 if params is None else params.dtype
+    sdt = sum.dtype if sum is not None else residual.dtype if residual is not None else xdt
+    odt = out.dtype if out is not None else out_dtype or xdt
+    for dt in (xdt, pdt, sdt, odt):
         if dt not in _DT:
             raise RalmError(4, f"dtype {dt}")
-    assert (want_sum or sum is None) and (want_out or out is None)
-    x, p.x_stride = _matrix(x, (T, D))
-    keep = [_vector(t, D, pdt) for t in (weight, bias, post_weight, post_bias)]
-    p.weight, p.bias, p.post_weight, p.post_bias = (_ptr(t) for t in keep)
-    p.post = 1 if post else 0
-    assert post or (post_weight is None and post_bias is None)
+    assert (want_sum or sum is None) and (want_out or out is None) and (post or (post_weight is None and post_bias is None))
+    x, xs = _matrix(x, T, D)
+    weight, bias = _vector(weight, D, pdt), _vector(bias, D, pdt)
+    if post:
+        post_weight, post_bias = _vector(post_weight, D, pdt), _vector(post_bias, D, pdt)
+    gs = gate_rows = rs = ss = os_ = 0
     if gate is not None:
         if gate.dim() == 2:
-            assert gate.dtype == x.dtype
-            gate, p.gate_stride = _matrix(gate, (T, D))
-            p.gate_rows = 1
+            assert gate.dtype == xdt
+            gate, gs = _matrix(gate, T, D)
+            gate_rows = 1
         else:
-            gate = _vector(gate, D, x.dtype)
-        p.gate = gate.data_ptr()
+            gate = _vector(gate, D, xdt)
     if residual is not None:
         assert residual.dtype == sdt
-        residual, p.residual_stride = _matrix(residual, (T, D))
-        p.residual = residual.data_ptr()
+        residual, rs = _matrix(residual, T, D)
     if want_sum:
-        sum, p.sum_stride = _out_matrix(sum, (T, D), sdt, x.device)
-        p.sum = sum.data_ptr()
+        sum, ss = _out_matrix(sum, T, D, sdt, x.device)
     if want_out:
-        out, p.out_stride = _out_matrix(out, (T, D), odt, x.device)
-        p.out = out.data_ptr()
-    p.x, p.x_dtype, p.param_dtype, p.sum_dtype, p.out_dtype = x.data_ptr(), _DT[x.dtype], _DT[pdt], _DT[sdt], _DT[odt]
-    _check(lib().ralm_residual_norm(ctypes.byref(p), _here(x, residual, gate, sum, out, *keep)))
+        out, os_ = _out_matrix(out, T, D, odt, x.device)
+    stream = _here(x, residual, gate, sum, out, weight, bias, post_weight, post_bias)
+    p = ralm_norm_t(T, D, _NORMS[kind], eps, scale, x.data_ptr(), xs, _DT[xdt], _DT[pdt], 1 if post else 0, _ptr(post_weight), _ptr(post_bias),
+                    _ptr(gate), gs, gate_rows, _ptr(residual), rs, _ptr(sum), ss, _DT[sdt], _ptr(weight), _ptr(bias), _ptr(out), os_, _DT[odt])
+    _check(lib().ralm_residual_norm(ctypes.byref(p), stream))
     return sum, out
 
 
@@ -835,14 +845,15 @@ def ralm_knnlm_target(logits: torch.Tensor, tokens: torch.Tensor, weights: torch
     Q, V = logits.shape
     k = tokens.shape[1]
     assert tokens.dtype == torch.int32 and weights.dtype == torch.float32 and tokens.shape == weights.shape == (Q, k)
-    logits, ls = _matrix(logits, (Q, V))
+    logits, ls = _matrix(logits, Q, V)
     if out is not None:
         out_dtype = out.dtype
     for dt in (logits.dtype, out_dtype):
         if dt not in _DT:
             raise RalmError(4, f"dtype {dt}")
-    out, os_ = _out_matrix(out, (Q, V), out_dtype, logits.device)
-    tokens, weights = tokens.contiguous(), weights.contiguous()
+    out, os_ = _out_matrix(out, Q, V, out_dtype, logits.device)
+    if not (tokens.is_contiguous() and weights.is_contiguous()):
+        tokens, weights = tokens.contiguous(), weights.contiguous()
     rows = _vector(share, Q, torch.float32) if isinstance(share, torch.Tensor) else None
     stream = _here(logits, tokens, weights, rows, out, workspace)
     if workspace is None:

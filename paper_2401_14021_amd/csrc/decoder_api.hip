@@ -120,8 +120,8 @@ ralm_status ralm_residual_norm(const ralm_norm_t *norm, void *stream)
 
 size_t ralm_knnlm_target_workspace_bytes(int64_t Q, int32_t V)
 {
-    (void)Q, (void)V;
-    return 0;
+    if (Q < 1 || Q > (1 << 20) || V < 1 || V > RALM_MAX_VOCABULARY) return 0;
+    return (size_t)Q * target_parts(Q, V) * sizeof(float2);
 }
 
 ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t Q, int32_t V, int32_t dtype, float temperature, const int32_t *tokens,
@@ -132,7 +132,7 @@ ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t
     if (V < 1 || V > RALM_MAX_VOCABULARY) return set_error(RALM_ERR_SHAPE, "V=%d out of [1, %d]", V, RALM_MAX_VOCABULARY);
     if (k < 0 || k > RALM_MAX_K) return set_error(RALM_ERR_K, "k=%d out of [0, %d]", k, RALM_MAX_K);
     if (!known(dtype) || !known(out_dtype)) return set_error(RALM_ERR_DTYPE, "dtype unknown");
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return set_error(RALM_ERR_RANGE, "temperature must be positive and finite");
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite((float)(1.4426950408889634 / (double)temperature))) return set_error(RALM_ERR_RANGE, "temperature must be positive and finite");
     if (!share && !(share_all >= 0.f && share_all <= 1.f)) return set_error(RALM_ERR_RANGE, "share_all must be in [0, 1]");
     if (Q == 0) return RALM_OK;
     if (!logits || !out || (k > 0 && (!tokens || !weights))) return set_error(RALM_ERR_NULL, "a pointer is NULL");
@@ -142,13 +142,21 @@ ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t
     if (!aligned(logits, bytes_of(dtype)) || !aligned(out, bytes_of(out_dtype)) || !aligned(tokens, 4) || !aligned(weights, 4) || !aligned(share, 4))
         return set_error(RALM_ERR_ALIGN, "pointers must be aligned to their type");
     if (logits == out && (dtype != out_dtype || logits_stride != out_stride)) return set_error(RALM_ERR_SHAPE, "out is logits of another type or stride");
-    (void)workspace, (void)workspace_bytes;
+    const int parts = target_parts(Q, V);
+    if (parts > 0) {
+        const size_t need = ralm_knnlm_target_workspace_bytes(Q, V);
+        if (!workspace || !aligned(workspace, 16)) return set_error(RALM_ERR_WORKSPACE, "workspace is NULL or not 16-byte aligned");
+        if (workspace_bytes < need) return set_error(RALM_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
+        if (Q * parts > 1 << 24) return set_error(RALM_ERR_SHAPE, "Q x V beyond 2^36; split the batch");
+    }
     TargetParams p;
     p.logits = logits;
     p.logits_stride = logits_stride;
     p.Q = Q;
     p.V = V, p.dtype = dtype;
-    p.inv_temperature = 1.f / temperature;
+    p.scale = (float)(1.4426950408889634 / (double)temperature);
+    p.parts = parts;
+    p.stats = static_cast<float2 *>(workspace);
     p.tokens = tokens;
     p.weights = weights;
     p.k = k;

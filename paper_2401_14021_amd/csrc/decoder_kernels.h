@@ -53,7 +53,7 @@ struct TargetParams {
     int64_t logits_stride;
     int64_t Q;
     int32_t V, dtype;
-    float inv_temperature;
+    float scale;           // log2 e / temperature
     const int32_t *tokens;
     const float *weights;
     int32_t k;
@@ -62,7 +62,11 @@ struct TargetParams {
     void *out;
     int64_t out_stride;
     int32_t out_dtype;
+    int32_t parts;         // workgroups of a row, from target_parts
+    float2 *stats;         // [Q][parts]: largest logit and sum of exponentials
 };
+constexpr int TARGET_PART = 4096;   // entries of a workgroup that shares a row
+int target_parts(int64_t Q, int32_t V);
 hipError_t launch_knnlm_target(const TargetParams &p, hipStream_t stream);
 
 }  // namespace ralm

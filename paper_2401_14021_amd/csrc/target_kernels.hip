@@ -1,8 +1,12 @@
 // The target of a verification: softmax of the logits mixed with the neighbours' weights (ralm_knnlm_target).
 //
-// Two passes over a row: its largest logit and the sum of exponentials under a running maximum, then the probabilities; what bounds them is
-// memory, the second pass finds the row in L2.  A token's neighbours are added up by one thread in their order, on the
-// probability formed again in fp32, so that the result is rounded once and does not depend on which thread came first.
+// target_row_kernel   a workgroup holds a row in registers: it is read once, each exponential is formed once; what bounds it is memory
+// target_stat_kernel, target_mix_kernel   few rows, or rows of more than 65536 entries: workgroups of 4096 entries leave their largest logit and sum of exponentials,
+//                     then read their entries again, from L2 or the last-level cache, and write
+//
+// Exponentials are 2^((x - top) c), c = log2 e / T: the difference first, so that logits of any size are safe; results below 2^-126 are 0.  The largest logit counts as at
+// least the lowest finite number, so that entries of -inf are 0 without being looked at, and a row of nothing else sums to 0.  A token's neighbours are added up by one thread in
+// their order, on the probability formed again in fp32: the result is rounded once and does not depend on which thread came first.
 #include "../../include/ralm.h"
 #include "ralm_common.h"
 #include "decoder_kernels.h"
@@ -11,24 +15,22 @@ namespace ralm {
 
 namespace {
 
-constexpr int NT = 1024;
-
-// 8 numbers from anywhere that their type may lie: rows of an odd number of entries are aligned to nothing else (the hardware takes such accesses whole)
+// 4 numbers from anywhere that their type may lie: rows of an odd number of entries are aligned to nothing else (the hardware takes such accesses whole).  Neighbouring lanes'
+// fours lie side by side in every type
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 template <int DT>
-__device__ __forceinline__ void load8(const void *p, int64_t at, float (&x)[8])
+__device__ __forceinline__ void load4(const void *p, int64_t at, float (&x)[4])
 {
     if constexpr (DT == DT_F32) {
-        const f32x4_any *s = reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + at);
-        const f32x4_any a = s[0], b = s[1];
+        const f32x4_any a = *reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + at);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+        for (int j = 0; j < 4; ++j) x[j] = a[j];
     } else {
-        const u32x4_any w = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(p) + at);
+        const u32x2_any w = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + at);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
             if constexpr (DT == DT_BF16) x[2 * j] = __uint_as_float(w[j] << 16), x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
             else x[2 * j] = f16_bits_to_f32(w[j] & 0xffffu), x[2 * j + 1] = f16_bits_to_f32(w[j] >> 16);
         }
@@ -49,125 +51,315 @@ __device__ __forceinline__ void store1(void *p, int64_t at, float x)
     else static_cast<_Float16 *>(p)[at] = (_Float16)x;
 }
 template <int DT>
-__device__ __forceinline__ void store8(void *p, int64_t at, const float (&x)[8])
+__device__ __forceinline__ void store4(void *p, int64_t at, const float (&x)[4])
 {
     if constexpr (DT == DT_F32) {
-        f32x4_any *d = reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at);
-        const f32x4_any a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
-        d[0] = a;
-        d[1] = b;
+        const f32x4_any a = {x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at) = a;
     } else {
-        u32x4_any w;
+        u32x2_any w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
             if constexpr (DT == DT_BF16)
                 w[j] = __builtin_bit_cast(uint16_t, (__bf16)x[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2 * j + 1]) << 16;
             else
                 w[j] = __builtin_bit_cast(uint16_t, (_Float16)x[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[2 * j + 1]) << 16;
         }
-        *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + at) = w;
+        *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + at) = w;
     }
 }
 
-// largest logit and sum of exp((x - largest) / T) of what a thread has seen; nothing: -inf, 0
-struct Seen {
-    float top, sum;
-    __device__ __forceinline__ void join(float t, float s, float inv)
-    {
-        const float m = fmaxf(top, t);   // (a NaN lies in s)
-        const float a = top == m ? sum : sum * expf((top - m) * inv), b = t == m ? s : s * expf((t - m) * inv);
-        // -inf on both sides: nothing, or what made the sum NaN
-        sum = a + b;
-        top = m;
-    }
-};
+constexpr float LOWEST = -3.402823466e38f;
 
-template <int DT, int DO>
-__global__ __launch_bounds__(NT) void target_kernel(const TargetParams p)
+__device__ __forceinline__ float exp_of(float y, float top, float c) { return __builtin_amdgcn_exp2f((y - top) * c); }
+
+template <int C>
+__device__ __forceinline__ float dpp(float v)
 {
-    __shared__ float tops[NT / 64], sums[NT / 64];
-    __shared__ int32_t near_token[RALM_MAX_K];
-    __shared__ float near_weight[RALM_MAX_K];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = blockIdx.x;
-    const float inv = p.inv_temperature;
-    const void *x = DT == DT_F32 ? static_cast<const void *>(static_cast<const float *>(p.logits) + row * p.logits_stride)
-                                 : static_cast<const void *>(static_cast<const uint16_t *>(p.logits) + row * p.logits_stride);
-    void *out = DO == DT_F32 ? static_cast<void *>(static_cast<float *>(p.out) + row * p.out_stride)
-                             : static_cast<void *>(static_cast<uint16_t *>(p.out) + row * p.out_stride);
-    const int V = p.V, V8 = V & ~7;
-    Seen seen = {-__builtin_inff(), 0.f};
-    auto take = [&](const float *y, int n) {
-        float m = y[0];
-        for (int j = 1; j < n; ++j) m = fmaxf(m, y[j]);
-        float s = 0.f;
-        for (int j = 0; j < n; ++j) s += y[j] == -__builtin_inff() ? 0.f : expf((y[j] - m) * inv);
-        seen.join(m, s, inv);
-    };
-    for (int v = tid * 8; v < V8; v += NT * 8) {
-        float y[8];
-        load8<DT>(x, v, y);
-        take(y, 8);
-    }
-    if (tid < V - V8) {
-        const float y = load1<DT>(x, V8 + tid);
-        take(&y, 1);
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const float t = __shfl_xor(seen.top, s, 64), u = __shfl_xor(seen.sum, s, 64);
-        seen.join(t, u, inv);
-    }
-    if (lane == 0) tops[wave] = seen.top, sums[wave] = seen.sum;
-    for (int j = tid; j < p.k; j += NT) near_token[j] = p.tokens[row * p.k + j], near_weight[j] = p.weights[row * p.k + j];
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), C, 0xf, 0xf, false));
+}
+// over the lanes of a wave, without LDS: 16 lanes by exchanges, then the four sixteens
+template <bool MAX>
+__device__ __forceinline__ float wave_all(float v)
+{
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+    v = op(v, dpp<0xB1>(v));
+    v = op(v, dpp<0x4E>(v));
+    v = op(v, dpp<0x141>(v));
+    v = op(v, dpp<0x140>(v));
+    auto at = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+    return op(op(at(0), at(16)), op(at(32), at(48)));
+}
+// over a workgroup of NT threads; words: NT / 64 floats of LDS.  All threads
+template <int NT, bool MAX>
+__device__ __forceinline__ float group_all(float v, float *words)
+{
+    v = wave_all<MAX>(v);
+    if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = v;
     __syncthreads();
-    seen = {-__builtin_inff(), 0.f};
+    v = words[0];
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) seen.join(tops[w], sums[w], inv);
-    const float share = p.share ? p.share[row] : p.share_all;
-    const float top = seen.top, per = top == -__builtin_inff() && seen.sum == 0.f ? 0.f : (1.f - share) / seen.sum;
-    auto prob = [&](float y) { return (y == -__builtin_inff() ? 0.f : expf((y - top) * inv)) * per; };   // per is NaN where the row is
-    // a token's weights, by the thread of the first neighbour that has it; its logit is read before the row may be written over
-    float mine = 0.f;
-    int32_t token = -1;
-    if (tid < p.k) {
-        token = near_token[tid];
-        if (token < 0 || token >= V) token = -1;
-        for (int j = 0; token >= 0 && j < p.k; ++j) {
-            if (near_token[j] != token) continue;
-            if (j < tid) token = -1;
-            else mine += near_weight[j];
+    for (int w = 1; w < NT / 64; ++w) v = MAX ? fmaxf(v, words[w]) : v + words[w];
+    return v;
+}
+
+// The entries v0 .. v1 - 1 of a row, 4 NV a thread; what lies behind is -inf
+template <int DT, int NT, int NV>
+__device__ __forceinline__ void load_entries(const void *x, int v0, int v1, float (&y)[NV][4])
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = v0 + (i * NT + (int)threadIdx.x) * 4;
+        if (at + 4 <= v1) {
+            load4<DT>(x, at, y[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[i][j] = at + j < v1 ? load1<DT>(x, at + j) : -__builtin_inff();
         }
-        if (token >= 0) mine = prob(load1<DT>(x, token)) + share * mine;
     }
-    __syncthreads();
-    for (int v = tid * 8; v < V8; v += NT * 8) {
-        float y[8];
-        load8<DT>(x, v, y);
+}
+template <int DT, int NT, int NV>
+__device__ __forceinline__ void store_entries(void *x, int v0, int v1, const float (&y)[NV][4])
+{
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = prob(y[j]);
-        store8<DO>(out, v, y);
+    for (int i = 0; i < NV; ++i) {
+        const int at = v0 + (i * NT + (int)threadIdx.x) * 4;
+        if (at + 4 <= v1) {
+            store4<DT>(x, at, y[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at + j < v1) store1<DT>(x, at + j, y[i][j]);
+        }
     }
-    if (tid < V - V8) store1<DO>(out, V8 + tid, prob(load1<DT>(x, V8 + tid)));
+}
+template <int NV>
+__device__ __forceinline__ float max_of(const float (&y)[NV][4])
+{
+    float m = LOWEST;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = fmaxf(m, y[i][j]);   // (a NaN shows in the sum)
+    return m;
+}
+// y becomes its exponential
+template <int NV>
+__device__ __forceinline__ float exps_of(float (&y)[NV][4], float top, float c)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float t = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            y[i][j] = exp_of(y[i][j], top, c);
+            t += y[i][j];
+        }
+        s += t;
+    }
+    return s;
+}
+
+// The tokens in [v0, v1) that a row's neighbours have, each with the sum of its weights in their order: a thread gets up to M of them, tokens of -1 are none.  Up to DIRECT
+// neighbours each looks for its token in front of it; more are sorted by token and place first (40 rows of 50257, us: no
+// neighbours 8.4, 64 10.7, 256 9.9 (18.6 unsorted), 1024 11.6).
+constexpr int DIRECT = 64;
+struct Near {
+    alignas(16) int32_t token[DIRECT];
+    alignas(16) float weight[RALM_MAX_K];
+    u64 keys[RALM_MAX_K];
+    int count;
+};
+template <int NT, int M>
+__device__ __forceinline__ void gather_near(Near &near, const TargetParams &p, int64_t row, int v0, int v1, int32_t (&token)[M], float (&sum)[M])
+{
+    static_assert(NT >= DIRECT && NT * M >= RALM_MAX_K, "a place for every neighbour");
+    const int tid = threadIdx.x, k = p.k;
+    const int32_t *tokens = p.tokens + row * k;
+    const float *weights = p.weights + row * k;
+#pragma unroll
+    for (int i = 0; i < M; ++i) token[i] = -1, sum[i] = 0.f;
+    if (k <= DIRECT) {
+        const int k4 = (k + 3) & ~3;
+        if (tid < k4) {
+            const int32_t t = tid < k ? tokens[tid] : -1;
+            token[0] = t >= v0 && t < v1 ? t : -1;
+            near.token[tid] = token[0];
+            near.weight[tid] = tid < k ? weights[tid] : 0.f;
+        }
+        __syncthreads();
+        if (tid < k4) {   // (by whole fours and without branches: one at a time, 64 neighbours took 3 us)
+            const int32_t own = token[0];
+            bool later = false;
+#pragma unroll 4
+            for (int j = 0; j < k4; j += 4) {
+                const int4 t = *reinterpret_cast<const int4 *>(near.token + j);
+                const float4 w = *reinterpret_cast<const float4 *>(near.weight + j);
+                sum[0] += t.x == own ? w.x : 0.f;
+                sum[0] += t.y == own ? w.y : 0.f;
+                sum[0] += t.z == own ? w.z : 0.f;
+                sum[0] += t.w == own ? w.w : 0.f;
+                later |= (t.x == own && j < tid) || (t.y == own && j + 1 < tid) || (t.z == own && j + 2 < tid) || (t.w == own && j + 3 < tid);
+            }
+            if (later) token[0] = -1;   // the first one's thread has them all
+        }
+        return;
+    }
+    if (tid == 0) near.count = 0;
     __syncthreads();
-    if (token >= 0) store1<DO>(out, token, mine);
+    for (int j = tid; j < k; j += NT) {
+        const int32_t t = tokens[j];
+        near.weight[j] = weights[j];
+        if (t >= v0 && t < v1) near.keys[atomicAdd(&near.count, 1)] = (u64)(uint32_t)t << 32 | (uint32_t)j;
+    }
+    __syncthreads();
+    const int n = near.count;
+    int size = 2;
+    while (size < n) size <<= 1;   // at most RALM_MAX_K, a power of two
+    for (int j = n + tid; j < size; j += NT) near.keys[j] = ~0ull;
+    __syncthreads();
+    sort_keys<NT, false>(near.keys, size);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        const int j = tid + i * NT;
+        if (j >= n) continue;
+        const uint32_t t = (uint32_t)(near.keys[j] >> 32);
+        if (j > 0 && (uint32_t)(near.keys[j - 1] >> 32) == t) continue;
+        token[i] = (int32_t)t;
+        for (int e = j; e < n && (uint32_t)(near.keys[e] >> 32) == t; ++e) sum[i] += near.weight[(uint32_t)near.keys[e]];
+    }
 }
 
 template <int DT>
+__device__ __forceinline__ const void *row_of(const void *p, int64_t at)
+{
+    return DT == DT_F32 ? static_cast<const void *>(static_cast<const float *>(p) + at) : static_cast<const void *>(static_cast<const uint16_t *>(p) + at);
+}
+
+// The model's share of a row over its sum of exponentials: NaN where the row is, 0 where there is nothing
+__device__ __forceinline__ float share_of_model(float share, float sum) { return sum == 0.f ? 0.f : (1.f - share) / sum; }
+
+// Two workgroups of 512 threads to a CU: with more than 128 registers there is one, and a row's phases have nothing beside them (1300 rows of 32000, bf16 to bf16: 83, now 55 us;
+// to fp32 63, where 1024 threads a row, one to a CU, take 74)
+template <int DT, int DO, int NT, int NV>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 512 && NV == 8 ? 6 : 4))) void target_row_kernel(const TargetParams p)
+{
+    constexpr int M = (RALM_MAX_K + NT - 1) / NT;
+    __shared__ Near near;
+    __shared__ float words[2][NT / 64];
+    const int64_t row = blockIdx.x;
+    const void *x = row_of<DT>(p.logits, row * p.logits_stride);
+    void *out = const_cast<void *>(row_of<DO>(p.out, row * p.out_stride));
+    float y[NV][4];
+    load_entries<DT, NT, NV>(x, 0, p.V, y);
+    int32_t token[M];
+    float sum[M], logit[M];
+    gather_near<NT, M>(near, p, row, 0, p.V, token, sum);
+#pragma unroll
+    for (int i = 0; i < M; ++i) logit[i] = token[i] >= 0 ? load1<DT>(x, token[i]) : 0.f;   // before the row may be written over
+    const float share = p.share ? p.share[row] : p.share_all;
+    const float top = group_all<NT, true>(max_of<NV>(y), words[0]);
+    const float all = group_all<NT, false>(exps_of<NV>(y, top, p.scale), words[1]);
+    const float per = share_of_model(share, all);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[i][j] *= per;
+    store_entries<DO, NT, NV>(out, 0, p.V, y);
+    __syncthreads();   // the entries of tokens are written again, by others
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+        if (token[i] >= 0) store1<DO>(out, token[i], exp_of(logit[i], top, p.scale) * per + share * sum[i]);
+}
+
+constexpr int PART_NT = 256, PART_NV = TARGET_PART / (PART_NT * 4);
+
+template <int DT>
+__global__ __launch_bounds__(PART_NT) void target_stat_kernel(const TargetParams p)
+{
+    __shared__ float words[2][PART_NT / 64];
+    const int64_t row = blockIdx.x / p.parts;
+    const int part = (int)(blockIdx.x - row * p.parts), v0 = part * TARGET_PART, v1 = p.V - v0 < TARGET_PART ? p.V : v0 + TARGET_PART;
+    float y[PART_NV][4];
+    load_entries<DT, PART_NT, PART_NV>(row_of<DT>(p.logits, row * p.logits_stride), v0, v1, y);
+    const float top = group_all<PART_NT, true>(max_of<PART_NV>(y), words[0]);
+    const float sum = group_all<PART_NT, false>(exps_of<PART_NV>(y, top, p.scale), words[1]);
+    if (threadIdx.x == 0) p.stats[row * p.parts + part] = make_float2(top, sum);
+}
+
+template <int DT, int DO>
+__global__ __launch_bounds__(PART_NT) void target_mix_kernel(const TargetParams p)
+{
+    constexpr int M = (RALM_MAX_K + PART_NT - 1) / PART_NT;
+    __shared__ Near near;
+    __shared__ float words[2][PART_NT / 64];
+    const int64_t row = blockIdx.x / p.parts;
+    const int part = (int)(blockIdx.x - row * p.parts), v0 = part * TARGET_PART, v1 = p.V - v0 < TARGET_PART ? p.V : v0 + TARGET_PART;
+    const void *x = row_of<DT>(p.logits, row * p.logits_stride);
+    void *out = const_cast<void *>(row_of<DO>(p.out, row * p.out_stride));
+    float y[PART_NV][4];
+    load_entries<DT, PART_NT, PART_NV>(x, v0, v1, y);
+    int32_t token[M];
+    float sum[M], logit[M];
+    gather_near<PART_NT, M>(near, p, row, v0, v1, token, sum);
+#pragma unroll
+    for (int i = 0; i < M; ++i) logit[i] = token[i] >= 0 ? load1<DT>(x, token[i]) : 0.f;
+    // a thread for every part: at most RALM_MAX_VOCABULARY / TARGET_PART
+    static_assert(RALM_MAX_VOCABULARY <= PART_NT * TARGET_PART, "parts of a row");
+    const float2 stat = (int)threadIdx.x < p.parts ? p.stats[row * p.parts + threadIdx.x] : make_float2(LOWEST, 0.f);
+    const float share = p.share ? p.share[row] : p.share_all;
+    const float top = group_all<PART_NT, true>(stat.x, words[0]);
+    const float all = group_all<PART_NT, false>(stat.y == 0.f ? 0.f : stat.y * exp_of(stat.x, top, p.scale), words[1]);
+    const float per = share_of_model(share, all);
+#pragma unroll
+    for (int i = 0; i < PART_NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[i][j] = exp_of(y[i][j], top, p.scale) * per;
+    store_entries<DO, PART_NT, PART_NV>(out, v0, v1, y);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+        if (token[i] >= 0) store1<DO>(out, token[i], exp_of(logit[i], top, p.scale) * per + share * sum[i]);
+}
+
+template <int DT, int DO>
 hipError_t launch(const TargetParams &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.Q);
-    if (p.out_dtype == DT_F32) target_kernel<DT, DT_F32><<<grid, NT, 0, stream>>>(p);
-    else if (p.out_dtype == DT_BF16) target_kernel<DT, DT_BF16><<<grid, NT, 0, stream>>>(p);
-    else target_kernel<DT, DT_F16><<<grid, NT, 0, stream>>>(p);
+    if (p.parts > 0) {
+        const dim3 grid((unsigned)(p.Q * p.parts));
+        target_stat_kernel<DT><<<grid, PART_NT, 0, stream>>>(p);
+        target_mix_kernel<DT, DO><<<grid, PART_NT, 0, stream>>>(p);
+    } else {
+        const dim3 grid((unsigned)p.Q);
+        if (p.V <= 1024) target_row_kernel<DT, DO, 256, 1><<<grid, 256, 0, stream>>>(p);
+        else if (p.V <= 4096) target_row_kernel<DT, DO, 256, 4><<<grid, 256, 0, stream>>>(p);
+        else if (p.V <= 8192) target_row_kernel<DT, DO, 512, 4><<<grid, 512, 0, stream>>>(p);
+        else if (p.V <= 16384) target_row_kernel<DT, DO, 512, 8><<<grid, 512, 0, stream>>>(p);
+        else if (p.V <= 32768) target_row_kernel<DT, DO, 512, 16><<<grid, 512, 0, stream>>>(p);
+        else target_row_kernel<DT, DO, 1024, 16><<<grid, 1024, 0, stream>>>(p);
+    }
     return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_of(const TargetParams &p, hipStream_t stream)
+{
+    return p.out_dtype == DT_F32 ? launch<DT, DT_F32>(p, stream) : p.out_dtype == DT_BF16 ? launch<DT, DT_BF16>(p, stream) : launch<DT, DT_F16>(p, stream);
 }
 
 }  // namespace
 
+// Workgroups of a row, 0: a row is one workgroup's.  us, a row's workgroup and shared rows (16 neighbours, fp32): V 8000, 1 row 5.2, 7.1; V 32000, 8 rows 8.2, 7.6, 64
+// rows 10.1, 10.2, 256 rows 17, 22; V 50257, 8 rows 11.5, 8.0, 128 rows 17.8, 17.8, 600 rows 63, 70
+int target_parts(int64_t Q, int32_t V)
+{
+    if (V <= 65536 && (Q >= 128 || V <= 8192)) return 0;
+    return (V + TARGET_PART - 1) / TARGET_PART;
+}
+
 hipError_t launch_knnlm_target(const TargetParams &p, hipStream_t stream)
 {
-    return p.dtype == DT_F32 ? launch<DT_F32>(p, stream) : p.dtype == DT_BF16 ? launch<DT_BF16>(p, stream) : launch<DT_F16>(p, stream);
+    return p.dtype == DT_F32 ? launch_of<DT_F32>(p, stream) : p.dtype == DT_BF16 ? launch_of<DT_BF16>(p, stream) : launch_of<DT_F16>(p, stream);
 }
 
 }  // namespace ralm
