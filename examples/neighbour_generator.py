@@ -5,7 +5,8 @@ holds the decoder's own hidden states over a corpus and the tokens that followed
 its pages are forked.  A round then
 
 1. looks the current state up in the request's speculation cache and drafts the tokens that followed the entry that it finds,
-2. reserves room (copying pages that are still shared), appends the drafts' keys and values in 4 bits and attends,
+2. reserves room (copying pages that are still shared) and runs the decoder on the drafts: norms of the residual stream, products with their epilogues,
+   keys turned by their places on the way into the 4-bit cache, attention,
 3. retrieves the neighbours of every state exactly, and mixes their distribution with the decoder's,
 4. verifies the drafts against that target from given random numbers,
 5. rolls the context back behind the last accepted one and updates the speculation cache.
@@ -16,6 +17,7 @@ from __future__ import annotations
 
 import os
 import sys
+from typing import Optional
 
 import torch
 
@@ -34,7 +36,8 @@ class Decoder:
         g = torch.Generator(device="cuda").manual_seed(seed)
 
         def weights(n, m):
-            return (torch.randn(n, m, generator=g, device="cuda") * n ** -0.5).bfloat16()
+            """[m, n]: a row for every output."""
+            return (torch.randn(n, m, generator=g, device="cuda") * n ** -0.5).bfloat16().t().contiguous()
 
         self.V, self.width, self.layers, self.H, self.Hkv, self.d = vocabulary, width, layers, heads, kv_heads, 64
         self.window, self.sinks = window, sinks
@@ -43,34 +46,33 @@ class Decoder:
         self.out = [weights(heads * 64, width) for _ in range(layers)]
         self.mlp = [(weights(width, 4 * width), weights(4 * width, width)) for _ in range(layers)]
         self.head = weights(width, vocabulary)
+        self.freqs = B.ralm_rotary_frequencies(64)
 
     def cache(self, requests: int, tokens: int, pages: int) -> B.KVCache:
         return B.KVCache.empty(requests, tokens, pages, n_layers=self.layers, n_heads=self.Hkv, d=self.d, page_tokens=16)
 
-    def run(self, kv: B.KVCache, tokens: torch.Tensor, places: torch.Tensor, offsets: torch.Tensor, max_q: int, max_len: int):
-        """The requests' last tokens (room for them is reserved): hidden states and logits of each, fp32."""
+    def run(self, kv: B.KVCache, tokens: torch.Tensor, places: Optional[torch.Tensor], offsets: torch.Tensor, max_q: int, max_len: int):
+        """The requests' last tokens (room for them is reserved): hidden states and logits of each, fp32.  ``places``: where they stand in their
+        texts; None: where they stand in the cache."""
         n = tokens.shape[0]
-        x = self.embed[tokens.long()].float()
-        angle = places.float().unsqueeze(1) * (10000.0 ** (-torch.arange(32, device="cuda") / 32.0))
-        cos, sin = angle.cos().unsqueeze(1), angle.sin().unsqueeze(1)
+        shift = None
+        if places is not None:
+            first, end = offsets[:-1], offsets[1:]
+            shift = (places[first.clamp(max=n - 1)] - (kv.lens - (end - first))).to(torch.int32)
 
-        def turned(y):
-            a, b = y.float().chunk(2, -1)
-            return torch.cat([a * cos - b * sin, a * sin + b * cos], -1).bfloat16()
+        def normed(x):
+            return B.ralm_residual_norm(x, want_sum=False, out_dtype=torch.bfloat16)[1]
 
-        def normed(y):
-            return (y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6)).bfloat16()
-
+        x = self.embed[tokens.long()].float()                                    # the residual stream
         for i in range(self.layers):
-            y = (normed(x) @ self.qkv[i]).view(n, -1, 64)
-            q, k, v = y.split([self.H, self.Hkv, self.Hkv], 1)
-            B.ralm_kv_append(kv, i, turned(k), v, offsets)
-            y = B.ralm_kv_attention(kv, i, turned(q), offsets, max_q=max_q, max_len=max_len, window=self.window, sinks=self.sinks)
-            x = x + (y.view(n, -1) @ self.out[i]).float()
+            q, k, v = B.ralm_linear(normed(x), self.qkv[i]).view(n, -1, 64).split([self.H, self.Hkv, self.Hkv], 1)
+            q = B.ralm_kv_append_rotary(kv, i, q, k, v, offsets, self.freqs, shift=shift)
+            y = B.ralm_kv_attention(kv, i, q, offsets, max_q=max_q, max_len=max_len, window=self.window, sinks=self.sinks)
+            B.ralm_linear(y.view(n, -1), self.out[i], residual=x, out=x)
             up, down = self.mlp[i]
-            x = x + (torch.relu(normed(x) @ up) @ down).float()
+            B.ralm_linear(B.ralm_linear(normed(x), up, act="relu"), down, residual=x, out=x)
         state = normed(x)
-        return state.float().contiguous(), (state @ self.head).float()
+        return state.float(), B.ralm_linear(state, self.head, out_dtype=torch.float32)
 
 
 class Generator:
@@ -90,7 +92,7 @@ class Generator:
         tokens = torch.where(torch.rand(corpus, generator=self.gen, device="cuda") < 0.1, noise, tokens)
         book = model.cache(1, corpus, corpus // 16)
         B.ralm_kv_reserve(book, torch.tensor([corpus], dtype=torch.int32, device="cuda"))
-        states, _ = model.run(book, tokens, torch.arange(corpus, device="cuda"), torch.tensor([0, corpus], device="cuda"), corpus, corpus)
+        states, _ = model.run(book, tokens, None, torch.tensor([0, corpus], device="cuda"), corpus, corpus)
         self.values = torch.roll(tokens, -1).contiguous()
         self.store = B.Datastore.from_fp32(states)
         self.cache_ids = torch.full((requests, 256), -1, dtype=torch.int32, device="cuda")
@@ -105,13 +107,10 @@ class Generator:
         if not bool(granted.all()):
             raise RuntimeError("the cache has no room for these requests")
         off = torch.cumsum(torch.tensor([0] + counts, device="cuda"), 0)
-        row = torch.repeat_interleave(torch.arange(len(counts), device="cuda"), off[1:] - off[:-1], output_size=sum(counts))
-        places = (self.kv.lens.long() - off[1:])[row] + torch.arange(sum(counts), device="cuda")
-        states, logits = self.model.run(self.kv, tokens, places, off, max(counts), self.max_tokens)
+        states, logits = self.model.run(self.kv, tokens, None, off, max(counts), self.max_tokens)
         ids, scores = B.ralm_retrieve_topk_ex(states, self.store, self.k)
         near, weights, _, _ = B.ralm_knnlm_probs(ids, scores, self.values, temperature=4.0, want_top=False)
-        target = torch.softmax(logits * self.sharpness, -1) * (1.0 - self.share)
-        target.scatter_add_(1, near.clamp(min=0).long(), weights * self.share)
+        target = B.ralm_knnlm_target(logits, near, weights, self.share, temperature=1.0 / self.sharpness, out=logits)
         return states, target, ids, off
 
     def prompt(self, tokens: torch.Tensor):
