@@ -65,6 +65,7 @@ ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *
         return set_error(RALM_ERR_ALIGN, "x and w must be 16-byte aligned, their strides multiples of 8 elements");
     if (!aligned(out, bytes_of(out_dtype)) || !aligned(residual, bytes_of(out_dtype)) || !aligned(bias, 2))
         return set_error(RALM_ERR_ALIGN, "out, residual and bias must be aligned to their type");
+    if (out == x || out == w || out == bias) return set_error(RALM_ERR_SHAPE, "out is x, w or bias");
     if (residual == out && residual_stride != out_stride) return set_error(RALM_ERR_SHAPE, "residual is out with another stride");
     LinearPlan plan = linear_plan(T, N, K, gated);
     if (plan.parts > 1) {

@@ -23,7 +23,7 @@ struct LinearParams {
     int32_t out_dtype;
 };
 // weights x rows of a workgroup
-enum { LINEAR_FEW_16, LINEAR_FEW_32, LINEAR_128x64, LINEAR_128x128, LINEAR_256x192, LINEAR_256x256 };
+enum { LINEAR_FEW_16, LINEAR_FEW_32, LINEAR_64x64, LINEAR_128x64, LINEAR_128x128, LINEAR_256x192, LINEAR_256x256 };
 struct LinearPlan {
     int32_t form;
     int32_t parts, part_strips;   // of the depth: workgroups that share it, strips of 64 each

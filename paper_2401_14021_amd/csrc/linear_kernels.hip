@@ -245,8 +245,9 @@ __global__ __launch_bounds__(W * 64) void linear_few_kernel(const LinearParams p
 
 // ---- many rows: tiles through LDS ------------------------------------------------------------------
 //
-// A workgroup owns BM weights x BN rows of x and walks the depth in strips of 64 elements, which go from memory straight into LDS (a ring of two strips: the loads
-// that refill a strip's slot are issued once every wave has read its last operands from it).  Operand reads of a k-step travel under the multiplies of the one
+// A workgroup owns BM weights x BN rows of x and walks the depth in strips of 64 elements, which go from memory straight into LDS: a ring of S strips, 2 where LDS holds no more
+// and 3 for narrow tiles, which wait for memory (T 64, K 4096, N 6144, 128 x 64: 2 strips 20.3 us, 3 18.3, 4 18.1, 6 18.3).  The loads that refill a strip's slot are
+// issued once every wave has read its last operands from it.  Operand reads of a k-step travel under the multiplies of the one
 // before; the 16-byte chunks of a row are swizzled so that 16 rows' reads of a chunk are free of bank conflicts.
 //
 // Multiplies of 16 x 16 x 32: half the accumulator traffic of 32 x 32 x 16, 3 to 7 % faster in every tile (8192^3, 256 x 256: 804, 778 us).  8 waves of 128 x 64
@@ -276,7 +277,7 @@ __device__ __forceinline__ void wait_vmcnt()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <bool F16, bool GATED, bool OUT32, int WM, int WN, int TM, int TN>
+template <bool F16, bool GATED, bool OUT32, int WM, int WN, int TM, int TN, int S>
 __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearParams p, const LinearPlan plan, const int n_tiles, const int t_tiles)
 {
     constexpr int BM = WM * TM * 16, BN = WN * TN * 16, NW = WM * WN;
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     }
     auto touch = [&](int strip) __attribute__((always_inline)) {
         const unsigned char *at = touch_base + (int64_t)(strip < KT ? strip : KT - 1) * 128;   // every strip begins inside the rows
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds0 + 2 * STAGE + wave * 256), "v"(touch_voff), "s"(at) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds0 + S * STAGE + wave * 256), "v"(touch_voff), "s"(at) : "memory");
     };
     auto next = [&]() __attribute__((always_inline)) {
         wbase += 128;
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
         if constexpr (GATED) ubase += 128;
     };
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < S; ++s) {
         if (s < KT) {
             if (s == KT - 1 && tail) {
 #pragma unroll
@@ -413,18 +414,29 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // behind the loads of every strip there is one touch
+    // behind the loads of every strip there is one touch (of the first strips: one in all)
     if constexpr (TOUCH) touch(2);
-    if (KT > 1) wait_vmcnt<LPS + TOUCH>();
-    else wait_vmcnt<TOUCH>();
+    // waits until but `strips` strips' loads are complete, as far as that many are under way
+    auto wait_but = [&](int strips) __attribute__((always_inline)) {
+        if (strips >= S - 1) wait_vmcnt<(S - 1) * LPS + TOUCH>();
+        else if (S > 2 && strips == S - 2) wait_vmcnt<(S > 2 ? S - 2 : 0) * LPS + TOUCH>();
+        else if (S > 3 && strips == S - 3) wait_vmcnt<(S > 3 ? S - 3 : 0) * LPS + TOUCH>();
+        else if (S > 4 && strips == S - 4) wait_vmcnt<(S > 4 ? S - 4 : 0) * LPS + TOUCH>();
+        else if (S > 5 && strips == S - 5) wait_vmcnt<(S > 5 ? S - 5 : 0) * LPS + TOUCH>();
+        else wait_vmcnt<TOUCH>();
+    };
+    static_assert(S >= 2 && S <= 6 && (S - 1) * LPS + TOUCH < 64 && (S == 2 || !TOUCH), "loads under way");
+    wait_but(KT - 1 < S - 1 ? KT - 1 : S - 1);
     __syncthreads();
 #pragma unroll
     for (int idx = 0; idx < NR; ++idx) read(0, 0, 0, idx);
 
     int kt = 0;
     // One strip.  LOADS: the strip behind the next one is loaded; TAIL: it may end behind the rows; LAST: there is no next one
-    auto stage = [&](int slot, auto loads_tag, auto tail_tag, auto last_tag) __attribute__((always_inline)) {
+    int slot = 0;
+    auto stage = [&](auto loads_tag, auto tail_tag, auto last_tag) __attribute__((always_inline)) {
         constexpr bool LOADS = decltype(loads_tag)::value, LAST = decltype(last_tag)::value;
+        const int after = slot + 1 == S ? 0 : slot + 1;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             if constexpr (NW == 8) {
@@ -437,10 +449,11 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 acc[m / TN][m % TN] = mfma16<F16>(fa[cur][m / TN], fb[cur][m % TN], acc[m / TN][m % TN]);
-                if (m < NR && !(LAST && kk == 1)) read(cur ^ 1, kk == 1 ? slot ^ 1 : slot, kk ^ 1, m);
+                if (m < NR && !(LAST && kk == 1)) read(cur ^ 1, kk == 1 ? after : slot, kk ^ 1, m);
                 if (kk == 0 && m == RV && !LAST) {
-                    // the next strip is complete (nothing but a touch is under way behind its loads), and every wave has read this one
-                    wait_vmcnt<TOUCH>();
+                    // the next strip is complete (what is under way are the strips behind it, and a touch), and every wave has read this one
+                    if constexpr (LOADS) wait_vmcnt<(S - 2) * LPS + TOUCH>();
+                    else wait_but(KT - 2 - kt);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
@@ -458,17 +471,15 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
             if constexpr (TOUCH) touch(kt + 2 + AHEAD);
             next();
         }
+        slot = after;
     };
-    for (; kt < KT - 2 - (tail ? 1 : 0); ++kt) stage(kt & 1, std::true_type{}, std::false_type{}, std::false_type{});
-    if (kt < KT - 2) {
-        stage(kt & 1, std::true_type{}, std::true_type{}, std::false_type{});
+    for (; kt < KT - S - (tail ? 1 : 0); ++kt) stage(std::true_type{}, std::false_type{}, std::false_type{});
+    if (kt < KT - S) {
+        stage(std::true_type{}, std::true_type{}, std::false_type{});
         ++kt;
     }
-    if (kt < KT - 1) {
-        stage(kt & 1, std::false_type{}, std::false_type{}, std::false_type{});
-        ++kt;
-    }
-    stage(kt & 1, std::false_type{}, std::false_type{}, std::true_type{});
+    for (; kt < KT - 1; ++kt) stage(std::false_type{}, std::false_type{}, std::false_type{});
+    stage(std::false_type{}, std::false_type{}, std::true_type{});
     wait_vmcnt<0>();   // touches: before LDS is anybody else's
     __syncthreads();   // other waves read operands where the sums go
     // The sums by way of LDS, 32 rows of x at a time, so that a row's outputs leave side by side, and in a loop: written out for every register, the code below would be
@@ -538,13 +549,13 @@ hipError_t launch_few(const LinearParams &p, hipStream_t stream)
     kernel<<<dim3((unsigned)((n_tiles + 7) / 8 * 8 * t_tiles)), W * 64, lds, stream>>>(p, n_tiles, t_tiles);
     return hipGetLastError();
 }
-template <bool F16, bool GATED, bool OUT32, int WM, int WN, int TM, int TN>
+template <bool F16, bool GATED, bool OUT32, int WM, int WN, int TM, int TN, int S = 2>
 hipError_t launch_tile(const LinearParams &p, const LinearPlan &plan, hipStream_t stream)
 {
     constexpr int BM = WM * TM * 16, BN = WN * TN * 16, COLS = GATED ? BM / 2 : BM;
     const int64_t n_tiles = (p.N + COLS - 1) / COLS, t_tiles = (p.T + BN - 1) / BN;
-    const size_t ring = 2 * (size_t)(BM + BN) * 128 + (WM * WN == 8 ? 8 * 256 : 0), sums = (size_t)WM * WN * 32 * (TM * 16 + 4) * 4, lds = ring > sums ? ring : sums;
-    auto kernel = linear_tile_kernel<F16, GATED, OUT32, WM, WN, TM, TN>;
+    const size_t ring = S * (size_t)(BM + BN) * 128 + (WM * WN == 8 ? 8 * 256 : 0), sums = (size_t)WM * WN * 32 * (TM * 16 + 4) * 4, lds = ring > sums ? ring : sums;
+    auto kernel = linear_tile_kernel<F16, GATED, OUT32, WM, WN, TM, TN, S>;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (once != hipSuccess) return once;
     kernel<<<dim3((unsigned)((n_tiles * t_tiles * plan.parts + 7) / 8 * 8)), WM * WN * 64, lds, stream>>>(p, plan, (int)n_tiles, (int)t_tiles);
@@ -561,7 +572,8 @@ hipError_t launch(const LinearParams &p, const LinearPlan &plan, hipStream_t str
     switch (plan.form) {
     case LINEAR_FEW_16: return launch_few<F16, GATED, OUT32, GATED ? 2 : 1, 1, 8, 4>(p, stream);   // (gated: 16 gates and 16 that they multiply)
     case LINEAR_FEW_32: return launch_few<F16, GATED, OUT32, GATED ? 4 : 2, 1, 8, GATED ? 2 : 4>(p, stream);
-    case LINEAR_128x64: return launch_tile<F16, GATED, OUT32, 2, 2, 4, 2>(p, plan, stream);
+    case LINEAR_64x64: return launch_tile<F16, GATED, OUT32, 1, 2, 4, 2, 3>(p, plan, stream);
+    case LINEAR_128x64: return launch_tile<F16, GATED, OUT32, 2, 2, 4, 2, 3>(p, plan, stream);
     case LINEAR_128x128: return launch_tile<F16, GATED, OUT32, 2, 2, 4, 4>(p, plan, stream);
     case LINEAR_256x192: return launch_tile<F16, GATED, OUT32, 4, 2, 4, 6>(p, plan, stream);
     default: return launch_tile<F16, GATED, OUT32, 2, 4, 8, 4>(p, plan, stream);
@@ -580,23 +592,24 @@ hipError_t launch_of(const LinearParams &p, const LinearPlan &plan, hipStream_t 
 // Which form, and over how many workgroups the depth is split: the one that a simple model of the time (us) says is fastest.
 //
 //   few   a start, a wave's share of the strips, and what goes through the L1 caches (16 rows of x for every 16 or 32 weights)
-//   tiles a start; for every round of workgroups its strips, each as long as the latency of its loads, the multiplies of the workgroups that share a CU or
-//         the weights' way from memory, whichever is longest, and an epilogue; for parts a second launch and the way of their sums to memory and back
+//   tiles a start; for every round of workgroups its strips, each as long as the multiplies of the workgroups that share a CU, or as a latency and the weights' way from
+//         memory, whichever is longer, and an epilogue; for parts a second launch and the way of their sums to memory and back
 //
-// The constants are a fit to 2500 measured calls (K 256 to 16384, N 500 to 50257, T 1 to 4096, gated and not, 1 to 16 parts).  Over these sizes the form
-// that is taken is 2 % slower than the fastest one in the mean and 18 % at most (T 256, K 2048, N 500 gated: 13.6, 11.5 us).  What it decides between, for
-// instance, us: T 1, K = N = 1024: few 4.6, tiles 7.5; T 64, K 4096, N 6144: few 25, tiles of 128 x 64 in 1 part 41, in 8 parts 18; T 1387, K 4096,
-// N 6144: tiles of 128 x 128 100, of 256 x 192 74, of 256 x 256 90.
+// The constants are a fit to 3400 measured calls (K 256 to 16384, N 500 to 50257, T 1 to 4096, gated and not, 1 to 16 parts; weights from HBM where they are more than a
+// few MB).  Over these sizes the form that is taken is 1.5 % slower than the fastest one in the mean and 25 % at most (T 16, K 4096, N 6144: 18.2, 14.6 us).  What it
+// decides between, us: T 1, K = N = 1024: few 4.7, tiles 7.5; T 64, K 4096, N 6144: few 25, tiles of 128 x 64 in 4 parts 16.7; T 1387, K 4096, N 6144: tiles of
+// 128 x 128 100, of 256 x 192 74, of 256 x 256 85.
 LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
 {
     struct Tile {
         int32_t form, bm, bn, per_cu;
         float latency, multiply, epilogue;
     };
-    static const Tile tiles[] = {{LINEAR_128x64, 128, 64, 3, 0.72f, 0.435f, 1.2f},
-                                 {LINEAR_128x128, 128, 128, 2, 0.95f, 0.1f, 3.7f},
-                                 {LINEAR_256x192, 256, 192, 1, 1.14f, 1.08f, 4.9f},
-                                 {LINEAR_256x256, 256, 256, 1, 0.3f, 1.28f, 7.5f}};
+    static const Tile tiles[] = {{LINEAR_64x64, 64, 64, 3, 0.06f, 0.36f, 0.f},
+                                 {LINEAR_128x64, 128, 64, 2, 0.2f, 0.375f, 1.85f},
+                                 {LINEAR_128x128, 128, 128, 2, 0.83f, 0.54f, 2.f},
+                                 {LINEAR_256x192, 256, 192, 1, 0.6f, 1.17f, 6.3f},
+                                 {LINEAR_256x256, 256, 256, 1, 0.35f, 1.34f, 8.8f}};
     static const int32_t parts_of[] = {1, 2, 3, 4, 6, 8, 12, 16};
     constexpr int CUS = 256;
     const int64_t rows = (int64_t)N << gated;
@@ -612,28 +625,26 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
     if (T <= 256) {
         for (int f = 0; f < 2; ++f) {
             const int bm = f ? 32 : 16;
-            const float wgs = (float)(ceil_div(rows, bm) * ceil_div(T, 16));
-            const float load = wgs / 512.f;
+            const float wgs = (float)(ceil_div(rows, bm) * ceil_div(T, 16)), load = wgs / 512.f;
             consider(f ? LINEAR_FEW_32 : LINEAR_FEW_16, 1,
-                     2.25f + (float)ceil_div(strips, 8) * (f ? 1.49f : 0.88f) * (load > 1.f ? load : 1.f) + wgs * (float)(bm + 16) * (float)K * (2.f / 12.9e6f));
+                     1.2f + (float)ceil_div(strips, 8) * (f ? 0.99f : 0.5f) * (load > 1.f ? load : 1.f) + wgs * (float)(bm + 16) * (float)K * (2.f / 13.2e6f));
         }
     }
     for (const Tile &tile : tiles) {
         const int64_t t_tiles = ceil_div(T, tile.bn), all = ceil_div(rows, tile.bm) * t_tiles;
         const int64_t slots = CUS * tile.per_cu;
         auto strip = [&](int64_t wgs, int per_cu) {
-            const float m = per_cu * tile.multiply, w = (float)wgs / (float)t_tiles * tile.bm * (128.f / 7.2e6f);
-            const float x = tile.latency > m ? tile.latency : m;
-            return x > w ? x : w;
+            const float m = per_cu * tile.multiply, w = tile.latency + (float)wgs / (float)t_tiles * tile.bm * (128.f / 15.2e6f);
+            return m > w ? m : w;
         };
         for (int32_t parts : parts_of) {
             // at least two strips a part; sums of less than 2^31 numbers
             if (parts > 1 && (strips / parts < 2 || T * rows > (1LL << 31) / parts)) break;
             const int64_t wgs = all * parts, full = wgs / slots, rest = wgs - full * slots;
             const float n = (float)ceil_div(strips, parts);
-            float t = 6.2f + (float)full * (n * strip(slots, tile.per_cu) + tile.epilogue);
+            float t = 3.45f + (float)full * (n * strip(slots, tile.per_cu) + tile.epilogue);
             if (rest) t += n * strip(rest, (int)ceil_div(rest, CUS)) + tile.epilogue;
-            if (parts > 1) t += 3.f + (float)parts * (float)(T * rows) * (8.f / 4.5e6f);
+            if (parts > 1) t += 2.4f + (float)parts * (float)(T * rows) * (8.f / 6.75e6f);
             consider(tile.form, parts, t);
         }
     }

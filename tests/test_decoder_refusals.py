@@ -37,6 +37,7 @@ def test_linear(b):
     assert at(xs=68) == ALIGN and at(ws=68) == ALIGN and at(x=P + 8) == ALIGN and at(w=P + 2) == ALIGN
     assert at(out=P + 1) == ALIGN and at(out=P + 2, odt=F32) == ALIGN and at(res=P + 2, odt=F32) == ALIGN and at(bias=P + 1) == ALIGN
     assert at(res=2 * P, rs=136) == SHAPE                                  # in place with another stride
+    assert at(out=P) == SHAPE and at(x=3 * P, out=P) == SHAPE and at(bias=2 * P) == SHAPE   # other inputs in place
     assert at(T=0, x=None, w=None, out=None) == 0
     need = L.ralm_linear_workspace_bytes(4, 128, 64, 0)
     assert L.ralm_linear_workspace_bytes(4, 128, 60, 0) == 0 and need >= 0
