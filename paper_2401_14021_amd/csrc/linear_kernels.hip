@@ -250,14 +250,15 @@ __global__ __launch_bounds__(W * 64) void linear_few_kernel(const LinearParams p
 // issued once every wave has read its last operands from it.  Operand reads of a k-step travel under the multiplies of the one
 // before; the 16-byte chunks of a row are swizzled so that 16 rows' reads of a chunk are free of bank conflicts.
 //
-// Multiplies of 16 x 16 x 32: half the accumulator traffic of 32 x 32 x 16, 3 to 7 % faster in every tile (8192^3, 256 x 256: 804, 778 us).  8 waves of 128 x 64
+// Multiplies of 16 x 16 x 32: half the accumulator traffic of 32 x 32 x 16, 3 to 7 % faster in every tile (8192^3, 256 x 256: 804, 778 us at the time).  8 waves of 128 x 64
 // each are faster than 4 of 128 x 128, whose SIMDs have nothing else to do at a rendezvous (778, 828).  Of 778 us the loads take 92 (timed with the strips left
 // where they are: 686), the operand reads some 45 more.
 #define RALM_LDS __attribute__((address_space(3)))
 #define RALM_SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-// slot of a row's chunk c: c ^ swizzle(row)
-__device__ __forceinline__ int swizzle(int row) { return (row ^ ((row & 15) >> 3)) & 7; }
+// slot of a row's chunk c: c ^ swizzle(row).  (Free of conflicts for 16 rows x 4 chunks a read; with bit 3 of the row folded in, as 32 rows x 2 chunks
+// like it, the LDS worked twice as long: 8192^3 784 us, now 766.)
+__device__ __forceinline__ int swizzle(int row) { return row & 7; }
 
 // what a load of a chunk behind the end of a row reads
 __device__ const uint4 zero_chunk = {0u, 0u, 0u, 0u};
