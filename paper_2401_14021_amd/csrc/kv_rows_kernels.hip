@@ -311,173 +311,163 @@ __device__ __forceinline__ void store_eight(void *p, int64_t at, const Eight<DT>
     }
 }
 
-// A workgroup takes TOK tokens: their places, the angles' cosines and sines into LDS once for all heads, then queries, keys and values.
-// WHOLE: pairs lie in pieces of 8 that are loaded whole (half a multiple of 8, or of 4 interleaved); otherwise pair by pair.
-template <int D, int DT, int TOK, bool WHOLE>
+// A workgroup takes a token: its place and the cosines and sines of its angles, once for all heads, while the first of its queries, keys and values are under way;
+// then all of them.  12018 tokens of 32 + 8 heads of 128, bf16: 56 us, 4.6 TB/s (59 with loads behind the place and the angles); 64 tokens 5.0, the chain of
+// offsets, length, page and angle.
+// WHOLE: partners lie in pieces of 8 that are loaded whole (interleaved ones in the same piece, others where half is a multiple of 8); otherwise pair by pair, which
+// takes 2.4 times as long.
+template <int D, int DT, bool WHOLE, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows rows, KvRotary p)
 {
     constexpr int C = D / 8;   // pieces of a head
-    __shared__ double2 turns[TOK][D / 2];
-    __shared__ uint8_t *tile_at[TOK];
-    __shared__ int64_t place[TOK];
-    __shared__ int row_at[TOK], is_owned[TOK];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ double2 turns[D / 2];
+    const int tid = threadIdx.x;
     // tokens beside each other on one XCD, as in the append
     const uint32_t per = (gridDim.x + 7) / 8, b = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
-    const int64_t t0 = (int64_t)b * TOK;
+    const int64_t t = b;
+    if (t >= rows.n) return;
+    static_assert(WHOLE || !INTERLEAVED, "interleaved pairs lie in whole pieces");
     const int half = p.half;
-    if (wave < TOK) {
-        const int64_t t = t0 + wave;
-        int row = 0, r = 0;
-        int64_t at = 0;
-        bool owned = false;
-        uint8_t *tile = t < rows.n ? place_of(kv, rows, t, row, owned, r, at) : nullptr;
-        if (owned && p.shift) at += p.shift[r];
-        if (lane == 0) tile_at[wave] = tile, place[wave] = at, row_at[wave] = row, is_owned[wave] = owned;
-    }
-    __syncthreads();
-    for (int i = tid; i < TOK * half; i += 256) {
-        const int k = i / half, j = i - k * half;
-        double c, s;
-        sincos((double)place[k] * p.freqs[j], &s, &c);
-        turns[k][j] = make_double2(c * p.amplitude, s * p.amplitude);
-    }
-    __syncthreads();
-    for (int k = 0; k < TOK; ++k) {
-        if (!is_owned[k]) continue;
-        const int64_t t = t0 + k;
-        if (p.q) {
-            const int64_t in = t * p.q_token, to = t * p.o_token;
-            if constexpr (WHOLE) {
-                if (p.interleaved) {
-                    for (int i = tid; i < p.n_q_heads * C; i += 256) {
-                        const int h = i / C, c = i % C;
-                        Eight<DT> x;
-                        x.load(p.q, in + h * p.q_head + 8 * c);
-                        if (8 * c < 2 * half) {
-                            double y[8];
+
+    // Queries by units: a piece of the lower half with its partner in the upper one, then pieces that do not turn; interleaved, every piece by itself
+    const int low = INTERLEAVED ? 0 : half / 8, units = WHOLE ? C - low : D - half, q_units = p.n_q_heads * units;
+    auto load_q = [&](int i, Eight<DT> &x, Eight<DT> &z) __attribute__((always_inline)) {
+        const int h = i / units, c = i - h * units;
+        const int64_t in = t * p.q_token + h * p.q_head;
+        x.load(p.q, in + 8 * (c < low ? c : c + low));
+        if (c < low) z.load(p.q, in + 8 * c + half);
+    };
+    auto finish_q = [&](int i, Eight<DT> &x, Eight<DT> &z) __attribute__((always_inline)) {
+        const int h = i / units, c = i - h * units;
+        const int64_t to = t * p.o_token + h * p.o_head;
+        if constexpr (INTERLEAVED) {
+            if (8 * c < 2 * half) {
+                double y[8];
 #pragma unroll
-                            for (int j = 0; j < 8; j += 2) {
-                                const double2 cs = turns[k][4 * c + j / 2];
-                                const double u = number_of<DT>(x, j), v = number_of<DT>(x, j + 1);
-                                y[j] = u * cs.x - v * cs.y;
-                                y[j + 1] = v * cs.x + u * cs.y;
-                            }
-                            pack<DT>(x, y);
-                        }
-                        store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c, x);
-                    }
-                } else {
-                    // a piece of the lower half together with its partner in the upper one; pieces that do not turn by themselves
-                    const int low = half / 8, units = C - low;
-                    for (int i = tid; i < p.n_q_heads * units; i += 256) {
-                        const int h = i / units, c = i - h * units;
-                        Eight<DT> x;
-                        if (c < low) {
-                            Eight<DT> z;
-                            x.load(p.q, in + h * p.q_head + 8 * c);
-                            z.load(p.q, in + h * p.q_head + 8 * c + half);
-                            double y[8], w[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const double2 cs = turns[k][8 * c + j];
-                                const double u = number_of<DT>(x, j), v = number_of<DT>(z, j);
-                                y[j] = u * cs.x - v * cs.y;
-                                w[j] = v * cs.x + u * cs.y;
-                            }
-                            pack<DT>(x, y);
-                            pack<DT>(z, w);
-                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c, x);
-                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * c + half, z);
-                        } else {
-                            x.load(p.q, in + h * p.q_head + 8 * (c + low));
-                            store_eight<DT>(p.q_out, to + h * p.o_head + 8 * (c + low), x);
-                        }
-                    }
+                for (int j = 0; j < 8; j += 2) {
+                    const bool turn = 4 * c + j / 2 < half;   // (a piece may hold the last pair and what does not turn)
+                    const double2 cs = turns[turn ? 4 * c + j / 2 : 0];
+                    const double u = number_of<DT>(x, j), v = number_of<DT>(x, j + 1);
+                    y[j] = turn ? u * cs.x - v * cs.y : u;
+                    y[j + 1] = turn ? v * cs.x + u * cs.y : v;
                 }
-            } else {
-                // pairs, then what does not turn
-                const int units = D - half;
-                for (int i = tid; i < p.n_q_heads * units; i += 256) {
-                    const int h = i / units, j = i - h * units;
-                    const int64_t a = in + h * p.q_head, o = to + h * p.o_head;
-                    if (j < half) {
-                        const int e0 = p.interleaved ? 2 * j : j, e1 = p.interleaved ? 2 * j + 1 : j + half;
-                        const double2 cs = turns[k][j];
-                        const double u = number<DT>(p.q, a + e0), v = number<DT>(p.q, a + e1);
-                        store_bits<DT>(p.q_out, o + e0, bits_of<DT>(u * cs.x - v * cs.y));
-                        store_bits<DT>(p.q_out, o + e1, bits_of<DT>(v * cs.x + u * cs.y));
-                    } else {
-                        store_bits<DT>(p.q_out, o + j + half, bits_of<DT>(number<DT>(p.q, a + j + half)));
-                    }
-                }
+                pack<DT>(x, y);
             }
+        } else if (c < low) {
+            double y[8], w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double2 cs = turns[8 * c + j];
+                const double u = number_of<DT>(x, j), v = number_of<DT>(z, j);
+                y[j] = u * cs.x - v * cs.y;
+                w[j] = v * cs.x + u * cs.y;
+            }
+            pack<DT>(x, y);
+            pack<DT>(z, w);
+            store_eight<DT>(p.q_out, to + 8 * c + half, z);
         }
-        uint8_t *at = tile_at[k];
-        if (!at) continue;
-        // keys: a lane turns its own piece, for which it reads the partners too; values go in as they are
-        const int row = row_at[k];
-        for (int i = tid; i < 2 * kv.n_heads * C; i += 256) {
-            const bool values = i >= kv.n_heads * C;
-            const int u = values ? i - kv.n_heads * C : i, h = u / C, c = u % C;
-            Eight<DT> x;
-            if (values) {
-                x.load(rows.v, t * rows.v_token + h * rows.v_head + 8 * c);
+        store_eight<DT>(p.q_out, to + 8 * (c < low ? c : c + low), x);
+    };
+    // Keys, each piece by itself with the partners that it needs read too, then values as they are
+    const int k_units = kv.n_heads * C;
+    auto load_kv = [&](int i, Eight<DT> &x, Eight<DT> &z) __attribute__((always_inline)) {
+        const bool values = i >= k_units;
+        const int u = values ? i - k_units : i, h = u / C, c = u % C;
+        const int64_t in = values ? t * rows.v_token + h * rows.v_head : t * rows.k_token + h * rows.k_head;
+        x.load(values ? rows.v : rows.k, in + 8 * c);
+        if (WHOLE && !INTERLEAVED && !values && 8 * c < 2 * half) z.load(rows.k, in + (8 * c < half ? 8 * c + half : 8 * c - half));
+    };
+    auto finish_kv = [&](int i, Eight<DT> &x, Eight<DT> &z, uint8_t *at, int row) __attribute__((always_inline)) {
+        const bool values = i >= k_units;
+        const int u = values ? i - k_units : i, h = u / C, c = u % C;
+        if (!values && 8 * c < 2 * half) {
+            double y[8];
+            if constexpr (WHOLE && INTERLEAVED) {
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    const bool turn = 4 * c + j / 2 < half;
+                    const double2 cs = turns[turn ? 4 * c + j / 2 : 0];
+                    const double e = number_of<DT>(x, j), f = number_of<DT>(x, j + 1);
+                    y[j] = turn ? e * cs.x - f * cs.y : e;
+                    y[j + 1] = turn ? f * cs.x + e * cs.y : f;
+                }
+            } else if constexpr (WHOLE) {
+                const bool lower = 8 * c < half;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const double2 cs = turns[(lower ? 8 * c : 8 * c - half) + j];
+                    const double e = number_of<DT>(x, j), f = number_of<DT>(z, j);
+                    y[j] = lower ? e * cs.x - f * cs.y : e * cs.x + f * cs.y;
+                }
             } else {
                 const int64_t in = t * rows.k_token + h * rows.k_head;
-                x.load(rows.k, in + 8 * c);
-                if (8 * c < 2 * half) {
-                    double y[8];
-                    if constexpr (WHOLE) {
-                        if (p.interleaved) {
 #pragma unroll
-                            for (int j = 0; j < 8; j += 2) {
-                                const double2 cs = turns[k][4 * c + j / 2];
-                                const double a = number_of<DT>(x, j), b2 = number_of<DT>(x, j + 1);
-                                y[j] = a * cs.x - b2 * cs.y;
-                                y[j + 1] = b2 * cs.x + a * cs.y;
-                            }
-                        } else {
-                            const bool low = 8 * c < half;
-                            Eight<DT> z;
-                            z.load(rows.k, in + (low ? 8 * c + half : 8 * c - half));
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const double2 cs = turns[k][(low ? 8 * c : 8 * c - half) + j];
-                                const double a = number_of<DT>(x, j), b2 = number_of<DT>(z, j);
-                                y[j] = low ? a * cs.x - b2 * cs.y : a * cs.x + b2 * cs.y;
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int e = 8 * c + j;
-                            const double a = number_of<DT>(x, j);
-                            y[j] = a;
-                            if (e < 2 * half) {
-                                const bool low = p.interleaved ? (e & 1) == 0 : e < half;
-                                const int other = p.interleaved ? e ^ 1 : low ? e + half : e - half;
-                                const double2 cs = turns[k][p.interleaved ? e >> 1 : low ? e : e - half];
-                                const double b2 = number<DT>(rows.k, in + other);
-                                y[j] = low ? a * cs.x - b2 * cs.y : a * cs.x + b2 * cs.y;
-                            }
-                        }
+                for (int j = 0; j < 8; ++j) {
+                    const int e = 8 * c + j;
+                    const double a = number_of<DT>(x, j);
+                    y[j] = a;
+                    if (e < 2 * half) {
+                        const bool lower = e < half;
+                        const double2 cs = turns[lower ? e : e - half];
+                        const double f = number<DT>(rows.k, in + (lower ? e + half : e - half));
+                        y[j] = lower ? a * cs.x - f * cs.y : a * cs.x + f * cs.y;
                     }
-                    pack<DT>(x, y);
                 }
             }
-            store_piece<D>(at + h * kv.head_bytes, values, row, c, x);
+            pack<DT>(x, y);
         }
+        store_piece<D>(at + h * kv.head_bytes, values, row, c, x);
+    };
+
+    Eight<DT> q0, q1, k0, k1;
+    if (WHOLE && tid < q_units) load_q(tid, q0, q1);
+    if (tid < 2 * k_units) load_kv(tid, k0, k1);
+    int row = 0, r = 0;
+    int64_t place = 0;
+    bool owned = false;
+    uint8_t *at = place_of(kv, rows, t, row, owned, r, place);   // every wave for itself
+    if (!owned) return;
+    if (p.shift) place += p.shift[r];
+    for (int j = tid; j < half; j += 256) {
+        double c, s;
+        sincos((double)place * p.freqs[j], &s, &c);
+        turns[j] = make_double2(c * p.amplitude, s * p.amplitude);
+    }
+    __syncthreads();
+    if constexpr (WHOLE) {
+        for (int i = tid; i < q_units; i += 256) {
+            if (i != tid) load_q(i, q0, q1);
+            finish_q(i, q0, q1);
+        }
+    } else {
+        // pairs, then what does not turn
+        for (int i = tid; i < q_units; i += 256) {
+            const int h = i / units, j = i - h * units;
+            const int64_t from = t * p.q_token + h * p.q_head, to = t * p.o_token + h * p.o_head;
+            if (j < half) {
+                const double2 cs = turns[j];
+                const double u = number<DT>(p.q, from + j), v = number<DT>(p.q, from + j + half);
+                store_bits<DT>(p.q_out, to + j, bits_of<DT>(u * cs.x - v * cs.y));
+                store_bits<DT>(p.q_out, to + j + half, bits_of<DT>(v * cs.x + u * cs.y));
+            } else {
+                store_bits<DT>(p.q_out, to + j + half, bits_of<DT>(number<DT>(p.q, from + j + half)));
+            }
+        }
+    }
+    if (!at) return;
+    for (int i = tid; i < 2 * k_units; i += 256) {
+        if (i != tid) load_kv(i, k0, k1);
+        finish_kv(i, k0, k1, at, row);
     }
 }
 
 template <int D, int DT>
 hipError_t rotary_of(const KvView &kv, const KvRows &rows, const KvRotary &p, hipStream_t stream)
 {
-    const bool whole = p.interleaved ? p.half % 4 == 0 : p.half % 8 == 0;
     const dim3 grid((unsigned)((rows.n + 7) / 8 * 8));
-    if (whole) kv_append_rotary_kernel<D, DT, 1, true><<<grid, 256, 0, stream>>>(kv, rows, p);
-    else kv_append_rotary_kernel<D, DT, 1, false><<<grid, 256, 0, stream>>>(kv, rows, p);
+    if (p.interleaved) kv_append_rotary_kernel<D, DT, true, true><<<grid, 256, 0, stream>>>(kv, rows, p);
+    else if (p.half % 8 == 0) kv_append_rotary_kernel<D, DT, true, false><<<grid, 256, 0, stream>>>(kv, rows, p);
+    else kv_append_rotary_kernel<D, DT, false, false><<<grid, 256, 0, stream>>>(kv, rows, p);
     return hipGetLastError();
 }
 template <int D>
