@@ -66,6 +66,34 @@ def test_whole_numbers_gated(b, T, N, K, dtype):
     assert torch.equal(b.ralm_linear(x, w, bias=bias, act="relu", gated=True, residual=res).double(), want + res.double())
 
 
+# sizes that reach every tile, with whole and broken strips, the depth in one part and in several
+TILES = [(259, 131, 64), (280, 129, 8), (286, 137, 768), (271, 137, 728), (194, 4761, 384), (133, 5493, 368), (20, 2209, 5888), (17, 2767, 4312),
+         (661, 7659, 128), (665, 7429, 72), (4489, 133, 3584), (2734, 157, 5048), (2083, 5817, 192), (3877, 2081, 248), (285, 7411, 3200),
+         (137, 5471, 5896), (1709, 8131, 384), (2718, 4465, 328), (3796, 1061, 3392), (1181, 3567, 3256)]
+TILES_GATED = [(259, 131, 64), (280, 129, 8), (24, 131, 6144), (21, 157, 5640), (72, 4291, 384), (69, 5105, 368), (18, 1725, 3904), (17, 1509, 4424),
+               (661, 3917, 128), (484, 5299, 72), (130, 1851, 5120), (1878, 147, 5384), (836, 4761, 256), (668, 8191, 136), (141, 5733, 2432),
+               (154, 5473, 2448), (4283, 1417, 384), (1183, 5497, 328), (1207, 1669, 3648), (194, 5641, 5304)]
+
+
+@pytest.mark.parametrize("T,N,K,gated", [(*s, False) for s in TILES] + [(*s, True) for s in TILES_GATED])
+def test_every_tile(b, T, N, K, gated):
+    """Whole numbers again, from operands whose rows lie apart with NaN between them: what is read behind a row's end would show."""
+    g = torch.Generator(device="cuda").manual_seed(T + N + K)
+    rows = 2 * N if gated else N
+    draw = lambda n, m, top: torch.randint(-top, top + 1, (n, m), generator=g, device="cuda").bfloat16()
+    x, w, bias, res = draw(T, K, 1), draw(rows, K, 1), draw(1, rows, 5)[0], draw(T, N, 99).float()
+    y = x.double() @ w.double().T.contiguous() + bias.double()
+    want = y[:, :N].clamp(min=0) * y[:, N:] if gated else y.clamp(min=0)
+    assert float(want.abs().max()) < 2 ** 23
+    big = torch.full((T + 1, N + 5), 7.0, device="cuda")
+    out = big[:T, 1:N + 1]
+    b.ralm_linear(pitched(x, 8), pitched(w, 24), bias=bias, act="relu", gated=gated, residual=res, out=out)
+    assert torch.equal(out.double(), want + res.double())
+    out.fill_(7.0)
+    assert bool((big == 7.0).all())
+    assert torch.equal(b.ralm_linear(x, w, bias=bias, act="relu", gated=gated), want.float().bfloat16())
+
+
 @pytest.mark.parametrize("T,N,K", [(1, 131, 72), (20, 77, 264), (64, 300, 136), (130, 259, 200), (520, 300, 520)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_strides(b, T, N, K, gated):
@@ -130,6 +158,17 @@ def test_activations(b, T, dtype, act, gated):
     assert bool(((got.double() - want).abs() <= tol).all())
     half = b.ralm_linear(x, w, bias=bias, act=act, gated=gated)                  # one rounding to 16 bits more
     assert bool(((half.double() - f).abs() <= tol + torch.finfo(dt).eps / 2 * (f.abs() + tol) + torch.finfo(dt).tiny * 2.0 ** -10).all())
+
+
+@pytest.mark.parametrize("T", [1, 70])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+def test_activations_far_out(b, T, act):
+    """Beyond every exponential's range an activation is its argument or nothing, and infinite where that is."""
+    x, w = torch.zeros(T, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(5, 64, dtype=torch.bfloat16, device="cuda")
+    x[:, 0], w[:, 0] = 1.0, torch.tensor([float("inf"), 1e30, 200.0, -1e30, -200.0])
+    got, sums = b.ralm_linear(x, w, act=act, out_dtype=torch.float32), w[:, 0].float()
+    assert torch.equal(got[:, :3], sums[:3].expand(T, -1))
+    assert torch.equal(got[:, 3:], (sums[3:] if act == "none" else torch.zeros(2, device="cuda")).expand(T, -1))
 
 
 @pytest.mark.parametrize("T", [1, 20, 64, 150, 400])
