@@ -698,11 +698,12 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
  *              stride), and must not overlap it otherwise
  *   out        device [T, N] of out_dtype (dtype or fp32); must not overlap x, w or bias
  *   workspace  ralm_linear_workspace_bytes(), 16-byte aligned (may be NULL where
- *              that is 0): sums of products that are split over workgroups
+ *              that is 0): sums of products that are split over workgroups.  Fewer rows are split further and
+ *              may need more: one workspace for several T has the largest size of theirs
  *
  * Strides of 0 are dense.  K is a multiple of 8 in [8, 2^17]; x and w are 16-byte
  * aligned and their strides multiples of 8 elements, at most 2^22; out, residual
- * and bias are aligned to their type.  T <= 2^22, N <= 2^20 (2^19 gated), T x N <= 2^36.
+ * and bias are aligned to their type.  T <= 2^22, N <= 2^20 (2^19 gated), T x N <= 2^36 (2^35).
  * Products are exact and summed in fp32, everything up to the one rounding to
  * out_dtype is fp32.  Results are the same from call to call; they may differ in
  * the last bits with T, which chooses how a sum is split.
@@ -733,7 +734,7 @@ ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *
  *   out        device [T, D] of out_dtype, or NULL (only s is wanted); may be x
  *
  * Apart from that outputs overlap no input and not each other.  Types are fp32, bf16 or fp16, pointers
- * aligned to them; strides in elements, 0 = dense.  1 <= D <= RALM_MAX_NORM, T <= 2^22.  Statistics and everything
+ * aligned to them; strides in elements, 0 = dense.  1 <= D <= RALM_MAX_NORM, T <= 2^22, T x D <= 2^36.  Statistics and everything
  * in between are fp32; the norm is taken of s before it is rounded.
  */
 enum { RALM_NORM_RMS = 0, RALM_NORM_LAYER = 1 };
@@ -809,12 +810,13 @@ ralm_status ralm_rotary_frequencies(double *freqs, int32_t rot, double base, dou
  *              [0, V) count for nothing.  0 <= k <= RALM_MAX_K
  *   share      device fp32 [Q] or NULL: share_all for every row
  *   out        device [Q, V] of out_dtype; may be logits itself (same type and stride)
- *   workspace  ralm_knnlm_target_workspace_bytes(), 16-byte aligned (may be NULL where that is 0)
+ *   workspace  ralm_knnlm_target_workspace_bytes() of Q or more rows, 16-byte aligned (may be NULL where that is 0)
  *
  * Sums and exponentials are fp32, a token's weights are added in the order of j, one
  * rounding to out_dtype.  Logits of -inf are probabilities of 0; a row of nothing
  * else has the neighbours' part alone.  +inf or NaN make their row NaN.  V <= RALM_MAX_VOCABULARY,
- * Q <= 2^20, Q x V <= 2^36 (2^20 rows of up to 65536 entries).  Probabilities below 2^-126 may be 0.
+ * Q <= 2^20; where V is more than 65536, Q x V, V rounded up to
+ * a multiple of 4096, is below 2^36.  Probabilities below 2^-126 may be 0.
  */
 size_t ralm_knnlm_target_workspace_bytes(int64_t Q, int32_t V);
 ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t Q, int32_t V, int32_t dtype,

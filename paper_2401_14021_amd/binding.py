@@ -707,7 +707,7 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 def alloc_linear_workspace(T: int, N: int, K: int, gated: bool = False, device="cuda") -> Optional[torch.Tensor]:
-    """For ralm_linear of up to T rows of these sizes; None where none is needed."""
+    """For ralm_linear of T rows of these sizes (fewer may need more); None where none is needed."""
     n = int(lib().ralm_linear_workspace_bytes(T, N, K, 1 if gated else 0))
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 

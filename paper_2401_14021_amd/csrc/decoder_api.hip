@@ -28,7 +28,7 @@ ralm_status check_linear(int64_t T, int32_t N, int32_t K, int32_t gated)
     if (T < 0 || T > MAX_ROWS) return set_error(RALM_ERR_SHAPE, "T=%lld out of [0, 2^22]", (long long)T);
     if (N < 1 || N > (1 << 20) >> gated) return set_error(RALM_ERR_SHAPE, "N=%d out of [1, 2^20] (2^19 gated)", N);
     if (K < 8 || K > MAX_K_LINEAR || K % 8) return set_error(RALM_ERR_SHAPE, "K=%d must be a multiple of 8 in [8, 2^17]", K);
-    if (T * N > 1LL << 36) return set_error(RALM_ERR_SHAPE, "T x N beyond 2^36; split the rows");
+    if (T * N > 1LL << (36 - gated)) return set_error(RALM_ERR_SHAPE, "T x N beyond 2^36 (2^35 gated); split the rows");
     return RALM_OK;
 }
 size_t sums_bytes(const LinearPlan &plan, int64_t T) { return plan.parts > 1 ? (size_t)plan.parts * T * plan.pitch * 4 : 0; }
@@ -94,6 +94,7 @@ ralm_status ralm_residual_norm(const ralm_norm_t *norm, void *stream)
     ralm_norm_t p = *norm;
     if (p.T < 0 || p.T > MAX_ROWS || p.D < 1 || p.D > RALM_MAX_NORM)
         return set_error(RALM_ERR_SHAPE, "T=%lld out of [0, 2^22] or D=%d out of [1, %d]", (long long)p.T, p.D, RALM_MAX_NORM);
+    if (p.T * p.D > 1LL << 36) return set_error(RALM_ERR_SHAPE, "T x D beyond 2^36; split the rows");
     if (p.kind != RALM_NORM_RMS && p.kind != RALM_NORM_LAYER) return set_error(RALM_ERR_RANGE, "kind=%d unknown", p.kind);
     if ((p.post != 0 && p.post != 1) || (p.gate && p.gate_rows != 0 && p.gate_rows != 1)) return set_error(RALM_ERR_RANGE, "post and gate_rows must be 0 or 1");
     if (!(p.eps >= 0.f) || !isfinite(p.eps) || !isfinite(p.scale)) return set_error(RALM_ERR_RANGE, "eps must not be negative, eps and scale finite");
@@ -116,13 +117,20 @@ ralm_status ralm_residual_norm(const ralm_norm_t *norm, void *stream)
         (p.sum && p.sum == p.x && (p.sum_stride != p.x_stride || p.sum_dtype != p.x_dtype)) ||
         (p.out && p.out == p.x && (p.out_stride != p.x_stride || p.out_dtype != p.x_dtype)))
         return set_error(RALM_ERR_SHAPE, "an output is an input of another type or stride");
+    for (const void *in : {p.gate, p.weight, p.bias, p.post_weight, p.post_bias}) {
+        if (in && (in == p.sum || in == p.out)) return set_error(RALM_ERR_SHAPE, "an output is the gate or a parameter");
+    }
     return launched(launch_residual_norm(p, static_cast<hipStream_t>(stream)));
 }
 
 size_t ralm_knnlm_target_workspace_bytes(int64_t Q, int32_t V)
 {
     if (Q < 1 || Q > (1 << 20) || V < 1 || V > RALM_MAX_VOCABULARY) return 0;
-    return (size_t)Q * target_parts(Q, V) * sizeof(float2);
+    // of up to Q rows: fewer of them may be split where many are not
+    size_t most = (size_t)Q * target_parts(Q, V);
+    const int64_t few = Q < TARGET_FEW ? Q : TARGET_FEW - 1;
+    if (few * target_parts(few, V) > (int64_t)most) most = (size_t)few * target_parts(few, V);
+    return most * sizeof(float2);
 }
 
 ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t Q, int32_t V, int32_t dtype, float temperature, const int32_t *tokens,
@@ -144,11 +152,11 @@ ralm_status ralm_knnlm_target(const void *logits, int64_t logits_stride, int64_t
         return set_error(RALM_ERR_ALIGN, "pointers must be aligned to their type");
     if (logits == out && (dtype != out_dtype || logits_stride != out_stride)) return set_error(RALM_ERR_SHAPE, "out is logits of another type or stride");
     const int parts = target_parts(Q, V);
+    if (Q * parts >= 1 << 24) return set_error(RALM_ERR_SHAPE, "Q x V beyond 2^36; split the batch");
     if (parts > 0) {
-        const size_t need = ralm_knnlm_target_workspace_bytes(Q, V);
+        const size_t need = (size_t)Q * parts * sizeof(float2);
         if (!workspace || !aligned(workspace, 16)) return set_error(RALM_ERR_WORKSPACE, "workspace is NULL or not 16-byte aligned");
         if (workspace_bytes < need) return set_error(RALM_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
-        if (Q * parts > 1 << 24) return set_error(RALM_ERR_SHAPE, "Q x V beyond 2^36; split the batch");
     }
     TargetParams p;
     p.logits = logits;

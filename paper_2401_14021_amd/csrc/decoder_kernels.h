@@ -66,6 +66,7 @@ struct TargetParams {
     float2 *stats;         // [Q][parts]: largest logit and sum of exponentials
 };
 constexpr int TARGET_PART = 4096;   // entries of a workgroup that shares a row
+constexpr int TARGET_FEW = 128;   // rows from which a workgroup takes one whole
 int target_parts(int64_t Q, int32_t V);
 hipError_t launch_knnlm_target(const TargetParams &p, hipStream_t stream);
 

@@ -353,7 +353,7 @@ hipError_t launch_of(const TargetParams &p, hipStream_t stream)
 // rows 10.1, 10.2, 256 rows 17, 22; V 50257, 8 rows 11.5, 8.0, 128 rows 17.8, 17.8, 600 rows 63, 70
 int target_parts(int64_t Q, int32_t V)
 {
-    if (V <= 65536 && (Q >= 128 || V <= 8192)) return 0;
+    if (V <= 65536 && (Q >= TARGET_FEW || V <= 8192)) return 0;
     return (V + TARGET_PART - 1) / TARGET_PART;
 }
 

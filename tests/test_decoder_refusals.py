@@ -29,7 +29,7 @@ def test_linear(b):
     assert at(x=None) == NULL and at(w=None) == NULL and at(out=None) == NULL
     assert at(T=-1) == SHAPE and at(T=(1 << 22) + 1) == SHAPE and at(N=0) == SHAPE and at(N=(1 << 20) + 1) == SHAPE
     assert at(N=(1 << 19) + 1, gated=1) == SHAPE and at(K=0) == SHAPE and at(K=12) == SHAPE and at(K=(1 << 17) + 8) == SHAPE
-    assert at(T=1 << 22, N=(1 << 14) + 1) == SHAPE
+    assert at(T=1 << 22, N=(1 << 14) + 1) == SHAPE and at(T=1 << 17, N=1 << 19, K=8, gated=1) == SHAPE   # 2^32 work-items
     assert at(dt=F32) == DTYPE and at(dt=7) == DTYPE and at(odt=F16) == DTYPE and at(odt=9) == DTYPE
     assert at(act=-1) == RANGE and at(act=5) == RANGE and at(gated=2) == RANGE
     assert at(xs=56) == SHAPE and at(ws=56) == SHAPE and at(os_=127) == SHAPE and at(res=P, rs=100) == SHAPE
@@ -67,6 +67,8 @@ def test_norm(b):
     assert at(out=2 * P) == SHAPE and at(residual=3 * P, sum=None, out_dtype=F32) == SHAPE
     assert at(residual=2 * P, residual_stride=72) == SHAPE                 # in place with another stride
     assert at(sum=P) == SHAPE and at(sum=P, sum_dtype=BF16, x_stride=72) == SHAPE and at(out=P, out_dtype=F32) == SHAPE and at(out=P, out_stride=72) == SHAPE
+    assert at(T=1 << 22, D=16392) == SHAPE                                 # 2^32 work-items
+    assert at(weight=2 * P) == SHAPE and at(bias=3 * P) == SHAPE and at(gate=2 * P, x=P) == SHAPE and at(post=1, post_weight=3 * P) == SHAPE
     assert at(T=0, x=None) == 0
 
 
@@ -111,6 +113,10 @@ def test_target(b):
     assert at(xs=99) == SHAPE and at(os_=99) == SHAPE and at(out=P, os_=104) == SHAPE and at(out=P, odt=BF16) == SHAPE
     assert at(x=P + 2) == ALIGN and at(out=P + 1, odt=BF16) == ALIGN and at(tok=P + 2) == ALIGN and at(w=P + 2) == ALIGN and at(share=P + 2) == ALIGN
     assert at(Q=0, x=None, out=None) == 0
+    assert at(Q=1 << 19, V=1 << 17) == SHAPE and at(Q=1 << 20, V=65537) == SHAPE   # 2^32 work-items
+    for V in (1000, 8193, 50257, 65536, 70000, 1 << 20):                   # room for Q rows is room for fewer
+        sizes = [L.ralm_knnlm_target_workspace_bytes(Q, V) for Q in (1, 2, 100, 127, 128, 129, 1000, 5000)]
+        assert sizes == sorted(sizes)
     need = L.ralm_knnlm_target_workspace_bytes(1, 1 << 20)
     if need:
         assert at(Q=1, V=1 << 20, work=None) == WORKSPACE and at(Q=1, V=1 << 20, work=P + 8) == WORKSPACE and at(Q=1, V=1 << 20, n=need - 1) == WORKSPACE
