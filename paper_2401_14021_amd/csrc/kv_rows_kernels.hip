@@ -294,12 +294,6 @@ __device__ __forceinline__ void pack(Eight<DT> &x, const double (&y)[8])
     }
 }
 template <int DT>
-__device__ __forceinline__ void store_bits(void *p, int64_t at, uint32_t b)
-{
-    if constexpr (DT == DT_F32) static_cast<uint32_t *>(p)[at] = b;
-    else static_cast<uint16_t *>(p)[at] = (uint16_t)b;
-}
-template <int DT>
 __device__ __forceinline__ void store_eight(void *p, int64_t at, const Eight<DT> &x)
 {
     if constexpr (DT == DT_F32) {
@@ -314,13 +308,14 @@ __device__ __forceinline__ void store_eight(void *p, int64_t at, const Eight<DT>
 // A workgroup takes a token: its place and the cosines and sines of its angles, once for all heads, while the first of its queries, keys and values are under way;
 // then all of them.  12018 tokens of 32 + 8 heads of 128, bf16: 56 us, 4.6 TB/s (59 with loads behind the place and the angles); 64 tokens 5.0, the chain of
 // offsets, length, page and angle.
-// WHOLE: partners lie in pieces of 8 that are loaded whole (interleaved ones in the same piece, others where half is a multiple of 8); otherwise pair by pair, which
-// takes 2.4 times as long.
+// WHOLE: partners lie in pieces of 8 that are loaded whole (interleaved ones in the same piece, others where half is a multiple of 8); otherwise 256 pieces at a time, whole
+// heads, meet in LDS, where a number finds its partner at any distance (half 50: 69 us, pair by pair from memory 136; 64 tokens 6.4, 9).
 template <int D, int DT, bool WHOLE, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows rows, KvRotary p)
 {
     constexpr int C = D / 8;   // pieces of a head
     __shared__ double2 turns[D / 2];
+    __shared__ uint32_t met[WHOLE ? 1 : 256 * (DT == DT_F32 ? 8 : 4)];
     const int tid = threadIdx.x;
     // tokens beside each other on one XCD, as in the append
     const uint32_t per = (gridDim.x + 7) / 8, b = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
@@ -330,7 +325,7 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows
     const int half = p.half;
 
     // Queries by units: a piece of the lower half with its partner in the upper one, then pieces that do not turn; interleaved, every piece by itself
-    const int low = INTERLEAVED ? 0 : half / 8, units = WHOLE ? C - low : D - half, q_units = p.n_q_heads * units;
+    const int low = WHOLE && !INTERLEAVED ? half / 8 : 0, units = C - low, q_units = p.n_q_heads * units;
     auto load_q = [&](int i, Eight<DT> &x, Eight<DT> &z) __attribute__((always_inline)) {
         const int h = i / units, c = i - h * units;
         const int64_t in = t * p.q_token + h * p.q_head;
@@ -380,9 +375,9 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows
     auto finish_kv = [&](int i, Eight<DT> &x, Eight<DT> &z, uint8_t *at, int row) __attribute__((always_inline)) {
         const bool values = i >= k_units;
         const int u = values ? i - k_units : i, h = u / C, c = u % C;
-        if (!values && 8 * c < 2 * half) {
+        if (WHOLE && !values && 8 * c < 2 * half) {
             double y[8];
-            if constexpr (WHOLE && INTERLEAVED) {
+            if constexpr (INTERLEAVED) {
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
                     const bool turn = 4 * c + j / 2 < half;
@@ -391,27 +386,13 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows
                     y[j] = turn ? e * cs.x - f * cs.y : e;
                     y[j + 1] = turn ? f * cs.x + e * cs.y : f;
                 }
-            } else if constexpr (WHOLE) {
+            } else {
                 const bool lower = 8 * c < half;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const double2 cs = turns[(lower ? 8 * c : 8 * c - half) + j];
                     const double e = number_of<DT>(x, j), f = number_of<DT>(z, j);
                     y[j] = lower ? e * cs.x - f * cs.y : e * cs.x + f * cs.y;
-                }
-            } else {
-                const int64_t in = t * rows.k_token + h * rows.k_head;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int e = 8 * c + j;
-                    const double a = number_of<DT>(x, j);
-                    y[j] = a;
-                    if (e < 2 * half) {
-                        const bool lower = e < half;
-                        const double2 cs = turns[lower ? e : e - half];
-                        const double f = number<DT>(rows.k, in + (lower ? e + half : e - half));
-                        y[j] = lower ? a * cs.x - f * cs.y : a * cs.x + f * cs.y;
-                    }
                 }
             }
             pack<DT>(x, y);
@@ -420,7 +401,7 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows
     };
 
     Eight<DT> q0, q1, k0, k1;
-    if (WHOLE && tid < q_units) load_q(tid, q0, q1);
+    if (tid < q_units) load_q(tid, q0, q1);
     if (tid < 2 * k_units) load_kv(tid, k0, k1);
     int row = 0, r = 0;
     int64_t place = 0;
@@ -440,19 +421,47 @@ __global__ __launch_bounds__(256) void kv_append_rotary_kernel(KvView kv, KvRows
             finish_q(i, q0, q1);
         }
     } else {
-        // pairs, then what does not turn
-        for (int i = tid; i < q_units; i += 256) {
-            const int h = i / units, j = i - h * units;
-            const int64_t from = t * p.q_token + h * p.q_head, to = t * p.o_token + h * p.o_head;
-            if (j < half) {
-                const double2 cs = turns[j];
-                const double u = number<DT>(p.q, from + j), v = number<DT>(p.q, from + j + half);
-                store_bits<DT>(p.q_out, to + j, bits_of<DT>(u * cs.x - v * cs.y));
-                store_bits<DT>(p.q_out, to + j + half, bits_of<DT>(v * cs.x + u * cs.y));
-            } else {
-                store_bits<DT>(p.q_out, to + j + half, bits_of<DT>(number<DT>(p.q, from + j + half)));
+        // x with its partners from the pieces of this pass, which begins with whole heads; all threads
+        auto turn = [&](Eight<DT> &x, bool turned, int c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (DT == DT_F32) met[8 * tid + j] = x.w[j];
+                else if (j < 4) met[4 * tid + j] = x.w[j];
             }
+            __syncthreads();
+            if (turned && 8 * c < 2 * half) {
+                const int head = 8 * (tid - c);
+                double y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int e = 8 * c + j;
+                    const bool lower = e < half, turns_too = e < 2 * half;
+                    const double2 cs = turns[lower ? e : turns_too ? e - half : 0];
+                    const double u = number_of<DT>(x, j), v = number<DT>(met, head + (lower ? e + half : turns_too ? e - half : e));
+                    y[j] = !turns_too ? u : lower ? u * cs.x - v * cs.y : u * cs.x + v * cs.y;
+                }
+                pack<DT>(x, y);
+            }
+            __syncthreads();
+        };
+        for (int i0 = 0; i0 < q_units; i0 += 256) {
+            const int i = i0 + tid, h = i / C, c = i % C;
+            if (i0 > 0 && i < q_units) load_q(i, q0, q1);
+            turn(q0, i < q_units, c);
+            if (i < q_units) store_eight<DT>(p.q_out, t * p.o_token + h * p.o_head + 8 * c, q0);
         }
+        for (int i0 = 0; i0 < k_units; i0 += 256) {
+            const int i = i0 + tid;
+            if (i0 > 0 && i < 2 * k_units) load_kv(i, k0, k1);
+            turn(k0, i < k_units, i % C);
+            if (at && i < 2 * k_units) finish_kv(i, k0, k1, at, row);
+        }
+        if (!at) return;
+        for (int i = (k_units + 255) / 256 * 256 + tid; i < 2 * k_units; i += 256) {   // values alone
+            load_kv(i, k0, k1);
+            finish_kv(i, k0, k1, at, row);
+        }
+        return;
     }
     if (!at) return;
     for (int i = tid; i < 2 * k_units; i += 256) {

@@ -82,6 +82,26 @@ def test_against_append_of_turned_keys(b, d, rot, inter, dtype):
         assert torch.equal(own, got) and torch.equal(kv.pages, want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot", [(64, 36), (128, 100), (256, 244), (256, 256), (256, 2)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_many_heads(b, d, rot, inter, dtype):
+    """Tokens of more pieces than a workgroup has threads, of queries and of keys; some of them without a place."""
+    H, Hq, n = 33, 71, 21
+    g = torch.Generator().manual_seed(rot)
+    q, k, v = (torch.randn(n, h, d, generator=g).to(DT[dtype]).cuda() for h in (Hq, H, H))
+    kv, freqs, off = setup(b, [19, 40], H, d), b.ralm_rotary_frequencies(rot), torch.tensor([0, 4, 20], device="cuda")
+    kv.table[1, 0] = -1                                                           # the first tokens of the second request
+    at = torch.tensor(list(range(15, 19)) + list(range(24, 40)) + [0], dtype=torch.float64, device="cuda")
+    b.ralm_kv_append(kv, 0, turned(k, at, freqs, inter, 1.0), v, off)
+    want = kv.pages.clone()
+    kv.pages.zero_()
+    out = torch.full_like(q, 7.0)
+    b.ralm_kv_append_rotary(kv, 0, q, k, v, off, freqs, interleaved=inter, q_out=out)
+    assert torch.equal(out[:20], turned(q, at, freqs, inter, 1.0)[:20]) and bool((out[20] == 7.0).all())
+    assert torch.equal(kv.pages, want) and bool(want.any())
+
+
 def test_far_places(b):
     """Places near 2^31: an angle of fp32 would be off by hundreds of turns' worth of steps."""
     kv = setup(b, [64], 2, 128)
