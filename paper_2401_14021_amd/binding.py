@@ -689,7 +689,7 @@ def _matrix(t: torch.Tensor, T: int, n: int) -> Tuple[torch.Tensor, int]:
 
 def _out_matrix(t: Optional[torch.Tensor], T: int, n: int, dtype: torch.dtype, device) -> Tuple[torch.Tensor, int]:
     if t is None:
-        return torch.empty((T, n), dtype=dtype, device=device), n
+        return torch.empty(T, n, dtype=dtype, device=device), n   # (of numbers, not a tuple: 0.4 us less)
     assert t.shape == (T, n) and t.dtype == dtype, f"{t.dtype} {tuple(t.shape)}, expected {dtype} {(T, n)}"
     a, b = t.stride()
     assert (b == 1 or n <= 1) and (a >= n or T <= 1), "an output's rows must lie side by side without overlap"
@@ -822,7 +822,7 @@ def ralm_kv_append_rotary(kv: KVCache, layer: int, q: Optional[torch.Tensor], k:
         n, heads, d = q.shape
         assert n == k.shape[0] and d == kv.d and q.dtype == k.dtype and qs[2] == 1
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty(n, heads, d, dtype=q.dtype, device=q.device)
         os_ = q_out.stride()
         assert q_out.shape == q.shape and q_out.dtype == q.dtype and os_[2] == 1 and not (0 in os_ and _repeats(q_out))
     _check(lib().ralm_kv_append_rotary(kv._ref, layer, _ptr(q), qs[0], qs[1], heads, _ptr(q_out), os_[0], os_[1], k.data_ptr(), v.data_ptr(),
