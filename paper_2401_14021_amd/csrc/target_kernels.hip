@@ -1,6 +1,6 @@
 // The target of a verification: softmax of the logits mixed with the neighbours' weights (ralm_knnlm_target).
 //
-// target_row_kernel   a workgroup holds a row in registers: it is read once, each exponential is formed once; what bounds it is memory
+// target_row_kernel   a workgroup holds a row in registers: it is read once; what bounds it is memory
 // target_stat_kernel, target_mix_kernel   few rows, or rows of more than 65536 entries: workgroups of 4096 entries leave their largest logit and sum of exponentials,
 //                     then read their entries again, from L2 or the last-level cache, and write
 //
@@ -118,20 +118,62 @@ __device__ __forceinline__ void load_entries(const void *x, int v0, int v1, floa
         }
     }
 }
+// 16-bit entries as they lie in memory, in half the registers; their exponentials are formed twice
+template <int DT, int NT, int NV>
+struct Packed {
+    u32x2_any w[NV];
+    __device__ __forceinline__ void load(const void *x, int n)
+    {
+        const uint16_t *from = static_cast<const uint16_t *>(x);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = (i * NT + (int)threadIdx.x) * 4;
+            if (at + 4 <= n) {
+                w[i] = *reinterpret_cast<const u32x2_any *>(from + at);
+            } else {
+                constexpr uint32_t NONE = DT == DT_BF16 ? 0xff80u : 0xfc00u;   // -inf
+                uint32_t b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = at + j < n ? from[at + j] : NONE;
+                w[i][0] = b[0] | b[1] << 16;
+                w[i][1] = b[2] | b[3] << 16;
+            }
+        }
+    }
+    // between two uses: the compiler would keep what it formed for the first one
+    __device__ __forceinline__ void anew()
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            uint32_t a = w[i][0], b = w[i][1];
+            asm("" : "+v"(a), "+v"(b));
+            w[i][0] = a;
+            w[i][1] = b;
+        }
+    }
+    __device__ __forceinline__ float at(int i, int j) const
+    {
+        const uint32_t v = w[i][j / 2];
+        if constexpr (DT == DT_BF16) return __uint_as_float(j & 1 ? v & 0xffff0000u : v << 16);
+        else return f16_bits_to_f32(j & 1 ? v >> 16 : v & 0xffffu);
+    }
+};
+template <int DT>
+__device__ __forceinline__ void store_four(void *x, int at, int end, const float (&y)[4])
+{
+    if (at + 4 <= end) {
+        store4<DT>(x, at, y);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (at + j < end) store1<DT>(x, at + j, y[j]);
+    }
+}
 template <int DT, int NT, int NV>
 __device__ __forceinline__ void store_entries(void *x, int v0, int v1, const float (&y)[NV][4])
 {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = v0 + (i * NT + (int)threadIdx.x) * 4;
-        if (at + 4 <= v1) {
-            store4<DT>(x, at, y[i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (at + j < v1) store1<DT>(x, at + j, y[i][j]);
-        }
-    }
+    for (int i = 0; i < NV; ++i) store_four<DT>(x, v0 + (i * NT + (int)threadIdx.x) * 4, v1, y[i]);
 }
 template <int NV>
 __device__ __forceinline__ float max_of(const float (&y)[NV][4])
@@ -240,10 +282,11 @@ __device__ __forceinline__ const void *row_of(const void *p, int64_t at)
 // The model's share of a row over its sum of exponentials: NaN where the row is, 0 where there is nothing
 __device__ __forceinline__ float share_of_model(float share, float sum) { return sum == 0.f ? 0.f : (1.f - share) / sum; }
 
-// Two workgroups of 512 threads to a CU: with more than 128 registers there is one, and a row's phases have nothing beside them (1300 rows of 32000, bf16 to bf16: 83, now 55 us;
-// to fp32 63, where 1024 threads a row, one to a CU, take 74)
+// Workgroups of 512 threads share a CU, so that a row's phases have others beside them: two of up to 128 registers, three where 16-bit entries are kept as they lie
+// (1300 rows of 32000, bf16 to fp32: a workgroup of 1024 threads, alone, 74, two 63, three 54 us, 4.6 TB/s; bf16 to bf16 55, 47.  Four spill: 68.  Shorter rows gain
+// nothing by it, and longer ones need 1024 threads' registers: 600 rows of 50257 52 us, packed 55.)
 template <int DT, int DO, int NT, int NV>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 512 && NV == 8 ? 6 : 4))) void target_row_kernel(const TargetParams p)
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 512 && (NV == 8 || (NV == 16 && DT != DT_F32)) ? 6 : 4))) void target_row_kernel(const TargetParams p)
 {
     constexpr int M = (RALM_MAX_K + NT - 1) / NT;
     __shared__ Near near;
@@ -251,22 +294,55 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 512 &&
     const int64_t row = blockIdx.x;
     const void *x = row_of<DT>(p.logits, row * p.logits_stride);
     void *out = const_cast<void *>(row_of<DO>(p.out, row * p.out_stride));
-    float y[NV][4];
-    load_entries<DT, NT, NV>(x, 0, p.V, y);
+    constexpr bool PACKED = DT != DT_F32 && NT == 512 && NV == 16;
+    float y[PACKED ? 1 : NV][4];
+    Packed<DT, NT, PACKED ? NV : 1> packed;
+    if constexpr (PACKED) packed.load(x, p.V);
+    else load_entries<DT, NT, NV>(x, 0, p.V, y);
     int32_t token[M];
     float sum[M], logit[M];
     gather_near<NT, M>(near, p, row, 0, p.V, token, sum);
 #pragma unroll
     for (int i = 0; i < M; ++i) logit[i] = token[i] >= 0 ? load1<DT>(x, token[i]) : 0.f;   // before the row may be written over
     const float share = p.share ? p.share[row] : p.share_all;
-    const float top = group_all<NT, true>(max_of<NV>(y), words[0]);
-    const float all = group_all<NT, false>(exps_of<NV>(y, top, p.scale), words[1]);
-    const float per = share_of_model(share, all);
+    float top, all, per;
+    if constexpr (PACKED) {
+        top = LOWEST;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[i][j] *= per;
-    store_entries<DO, NT, NV>(out, 0, p.V, y);
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, packed.at(i, j));   // (a NaN shows in the sum)
+        top = group_all<NT, true>(top, words[0]);
+        packed.anew();
+        all = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float t = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t += exp_of(packed.at(i, j), top, p.scale);
+            all += t;
+        }
+        all = group_all<NT, false>(all, words[1]);
+        packed.anew();
+        per = share_of_model(share, all);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = exp_of(packed.at(i, j), top, p.scale) * per;
+            store_four<DO>(out, (i * NT + (int)threadIdx.x) * 4, p.V, e);
+        }
+    } else {
+        top = group_all<NT, true>(max_of<NV>(y), words[0]);
+        all = group_all<NT, false>(exps_of<NV>(y, top, p.scale), words[1]);
+        per = share_of_model(share, all);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[i][j] *= per;
+        }
+        store_entries<DO, NT, NV>(out, 0, p.V, y);
+    }
     __syncthreads();   // the entries of tokens are written again, by others
 #pragma unroll
     for (int i = 0; i < M; ++i)

@@ -94,6 +94,28 @@ def test_masks_infinities_and_nan(b, V, dtype):
     assert bool(got[4].isnan().all()) and bool(got[5].isnan().all())
 
 
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("Q,V,k", [(128, 10_001, 16), (131, 16_385, 65), (130, 20_003, 100), (129, 32_768, 16), (128, 50_257, 5), (133, 65_535, 3)])
+def test_rows_of_one_workgroup(b, Q, V, k, dtype, out):
+    """Long rows, enough of them for one to be a workgroup's: masks and what is no number among them, rows that lie apart, in place."""
+    logits, tokens, weights, share = inputs(Q, V, k, dtype, V)
+    logits[1, :V // 2] = float("-inf")
+    logits[2] = float("-inf")
+    logits[3] = torch.finfo(DT[dtype]).min
+    logits[4, 5] = float("nan")
+    logits[5, V - 1] = float("inf")
+    rest = torch.tensor([i for i in range(Q) if i not in (4, 5)], device="cuda")
+    want, err = formula(logits[rest], tokens[rest], weights[rest], share[rest], 0.7)
+    big = torch.full((Q, V + 3), 7.0, dtype=DT[out], device="cuda")
+    got = b.ralm_knnlm_target(logits, tokens, weights, share, temperature=0.7, out=big[:, 1:V + 1])
+    assert near(got[rest], want, err) and bool(got[4:6].isnan().all())
+    if dtype == out:
+        own = logits.clone()
+        assert b.ralm_knnlm_target(own, tokens, weights, share, temperature=0.7, out=own) is own and torch.equal(own[rest], got[rest])
+    got.fill_(7.0)
+    assert bool((big == 7.0).all())
+
+
 def test_a_tokens_weights_add_up_in_order(b):
     """All neighbours are one token: the sum is that of fp32 additions in their order, call after call."""
     k = 1024
