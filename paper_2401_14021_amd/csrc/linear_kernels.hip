@@ -6,6 +6,8 @@
 //  linear_few_kernel   few rows, small weights: what bounds it is the latency of a launch and of one trip to memory
 //  linear_tile_kernel  tiles through LDS; few rows: bound by the weights' way from memory, the depth split over workgroups; many rows: by the matrix cores
 //  linear_join_kernel  sums of a split depth, and the epilogue
+#include <math.h>
+
 #include <type_traits>
 
 #include "../../include/ralm.h"
@@ -285,6 +287,7 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW, LPS = NA + NB;   // loads of a wave per strip, 8 rows each
     constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
     constexpr int COLS = GATED ? BM / 2 : BM, HALF = TM * 8;
+    constexpr bool TOUCH = NW == 8;
     constexpr int NM = TM * TN, NR = TM + TN;
     constexpr int RV = NR + 6 < NM ? NR + 6 : NM - 1;   // the rendezvous follows this multiply of a strip's first k-step
     constexpr int PLACES = NM - 1 - RV + NM - NR;   // multiplies that loads are issued behind: those of the first k-step after the rendezvous, those of the second after its reads
@@ -335,9 +338,13 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     const int strips = (p.K + 63) / 64, first = part * plan.part_strips;
     const int KT = strips - first < plan.part_strips ? strips - first : plan.part_strips;   // at least one
     const int tail = first + KT == strips ? p.K & 63 : 0;                                     // elements of the last strip, 0: all
-    wbase += (int64_t)first * 128;
-    xbase += (int64_t)first * 128;
-    ubase += (int64_t)first * 128;
+    // Few rows, whose x an XCD's L2 holds: neighbouring tiles begin at other strips of their part and go round, or rows that lie a power of two apart would keep a few
+    // channels of the memory busy at a time (weights from HBM, us: T 16, K 16384, N 4096 in 8 parts 42, 30; T 45, K 4096, 22528 gated rows 48.6, 43.7)
+    const int begin = !TOUCH && p.T * p.K <= 1 << 20 && !tail ? in / high * 13 % KT : 0;
+    int until = KT - begin;
+    wbase += (int64_t)(first + begin) * 128;
+    xbase += (int64_t)(first + begin) * 128;
+    ubase += (int64_t)(first + begin) * 128;
     // TAIL: the strip may end behind the rows
     auto issue = [&](int idx, int slot, auto tail_tag) __attribute__((always_inline)) {
         const bool is_a = idx < NA;
@@ -358,7 +365,6 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     // strips before its loads, to have them in this XCD's L2: one dword a line, into a corner of LDS that nobody reads; a quarter of the weights' rows by each of four
     // neighbours that share them, and of the rows of x likewise.  Weights from HBM, us: 1387 rows, K 4096, N 16384 186, 183 (256 x 256: 213, 200); 4096 rows 455, 428;
     // 8192 rows, K 16384, N 4096 835, 797.  Tiles of 128 x 128, which share CUs, lost 4 % by it.
-    constexpr bool TOUCH = NW == 8;
     constexpr int AHEAD = 2, ROWS_A = BM / 4 / (NW / 2), ROWS_B = BN / 4 / (NW / 2);   // rows that a wave touches
     const unsigned char *touch_base = xbase;
     uint32_t touch_voff = 0;
@@ -377,9 +383,10 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
         asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds0 + S * STAGE + wave * 256), "v"(touch_voff), "s"(at) : "memory");
     };
     auto next = [&]() __attribute__((always_inline)) {
-        wbase += 128;
-        xbase += 128;
-        if constexpr (GATED) ubase += 128;
+        const int64_t step = !TOUCH && --until == 0 ? 128 - KT * 128 : 128;
+        wbase += step;
+        xbase += step;
+        if constexpr (GATED) ubase += step;
     };
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -592,12 +599,12 @@ hipError_t launch_of(const LinearParams &p, const LinearPlan &plan, hipStream_t 
 
 // Which form, and over how many workgroups the depth is split: the one that a simple model of the time (us) says is fastest.
 //
-//   few   a start, a wave's share of the strips, and what goes through the L1 caches (16 rows of x for every 16 or 32 weights)
-//   tiles a start; for every round of workgroups its strips, each as long as the multiplies of the workgroups that share a CU, or as a latency and the weights' way from
-//         memory, whichever is longer, and an epilogue; for parts a second launch and the way of their sums to memory and back
+//   few   a start, a wave's share of the strips times what shares a CU, and what goes through the L1 caches (up to 16 rows of x for every 16 to 64 weights)
+//   tiles a start; for every round of workgroups its strips, each as long as the multiplies of the workgroups that share a CU, as a latency, or as the weights' way from
+//         memory, whichever is longest, and an epilogue; for parts a second launch and the way of their sums to memory and back
 //
-// The constants are a fit to 3400 measured calls (K 256 to 16384, N 500 to 50257, T 1 to 4096, gated and not, 1 to 16 parts; weights from HBM where they are more than a
-// few MB).  Over these sizes the form that is taken is 1.5 % slower than the fastest one in the mean and 25 % at most (T 16, K 4096, N 6144: 18.2, 14.6 us).  What it
+// The constants are a fit to 9000 measured calls (K 256 to 16384, N 500 to 50257, T 1 to 4096, gated and not, 1 to 16 parts; weights from HBM where they are more than a
+// few MB).  Over these sizes the form that is taken is 1.2 % slower than the fastest one in the mean and 24 % at most (T 16, K 6144, N 2048: 14.6, 11.8 us).  What it
 // decides between, us: T 1, K = N = 1024: few 4.7, tiles 7.5; T 64, K 4096, N 6144: few 25, tiles of 128 x 64 in 4 parts 16.7; T 1387, K 4096, N 6144: tiles of
 // 128 x 128 100, of 256 x 192 74, of 256 x 256 85.
 LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
@@ -606,9 +613,9 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
         int32_t form, bm, bn, per_cu;
         float latency, multiply, epilogue;
     };
-    static const Tile tiles[] = {{LINEAR_64x64, 64, 64, 3, 0.06f, 0.36f, 0.f},
-                                 {LINEAR_128x64, 128, 64, 2, 0.2f, 0.375f, 1.85f},
-                                 {LINEAR_128x128, 128, 128, 2, 0.83f, 0.54f, 2.f},
+    static const Tile tiles[] = {{LINEAR_64x64, 64, 64, 3, 0.35f, 0.364f, 1.48f},
+                                 {LINEAR_128x64, 128, 64, 2, 0.01f, 0.421f, 3.22f},
+                                 {LINEAR_128x128, 128, 128, 2, 0.95f, 0.53f, 3.02f},
                                  {LINEAR_256x192, 256, 192, 1, 0.6f, 1.17f, 6.3f},
                                  {LINEAR_256x256, 256, 256, 1, 0.35f, 1.34f, 8.8f}};
     static const int32_t parts_of[] = {1, 2, 3, 4, 6, 8, 12, 16};
@@ -624,18 +631,20 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
         if (plan.form < 0 || t < best) plan.form = form, plan.parts = parts, best = t;
     };
     if (T <= 256) {
+        static const float strip[] = {0.249f, 0.593f, 2.256f};   // of 16, 32, 64 weights
         for (int f = 0; f < 2; ++f) {
-            const int bm = f ? 32 : 16;
-            const float wgs = (float)(ceil_div(rows, bm) * ceil_div(T, 16)), load = wgs / 512.f;
+            const int kind = f + gated, bm = 16 << kind;
+            const float wgs = (float)(ceil_div(rows, bm) * ceil_div(T, 16)), load = wgs / 210.f;
             consider(f ? LINEAR_FEW_32 : LINEAR_FEW_16, 1,
-                     1.2f + (float)ceil_div(strips, 8) * (f ? 0.99f : 0.5f) * (load > 1.f ? load : 1.f) + wgs * (float)(bm + 16) * (float)K * (2.f / 13.2e6f));
+                     0.84f + (float)ceil_div(strips, 8) * strip[kind] * (load > 1.f ? load : 1.f) + wgs * (float)(bm + (T < 16 ? T : 16)) * (float)K * (2.f / 11.9e6f));
         }
     }
     for (const Tile &tile : tiles) {
         const int64_t t_tiles = ceil_div(T, tile.bn), all = ceil_div(rows, tile.bm) * t_tiles;
         const int64_t slots = CUS * tile.per_cu;
         auto strip = [&](int64_t wgs, int per_cu) {
-            const float m = per_cu * tile.multiply, w = tile.latency + (float)wgs / (float)t_tiles * tile.bm * (128.f / 15.2e6f);
+            const float m = per_cu * tile.multiply, bytes = (float)wgs / (float)t_tiles * tile.bm * 128.f;
+            const float w = fmaxf(tile.latency + bytes / 53.5e6f, bytes / 8.7e6f);
             return m > w ? m : w;
         };
         for (int32_t parts : parts_of) {
@@ -643,9 +652,9 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
             if (parts > 1 && (strips / parts < 2 || T * rows > (1LL << 31) / parts)) break;
             const int64_t wgs = all * parts, full = wgs / slots, rest = wgs - full * slots;
             const float n = (float)ceil_div(strips, parts);
-            float t = 3.45f + (float)full * (n * strip(slots, tile.per_cu) + tile.epilogue);
+            float t = 0.62f + (float)full * (n * strip(slots, tile.per_cu) + tile.epilogue);
             if (rest) t += n * strip(rest, (int)ceil_div(rest, CUS)) + tile.epilogue;
-            if (parts > 1) t += 2.4f + (float)parts * (float)(T * rows) * (8.f / 6.75e6f);
+            if (parts > 1) t += 2.92f + (float)parts * (float)(T * rows) * (8.f / 4.7e6f);
             consider(tile.form, parts, t);
         }
     }
