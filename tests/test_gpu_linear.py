@@ -69,10 +69,12 @@ def test_whole_numbers_gated(b, T, N, K, dtype):
 # sizes that reach every tile, with whole and broken strips, the depth in one part and in several
 TILES = [(259, 131, 64), (280, 129, 8), (286, 137, 768), (271, 137, 728), (194, 4761, 384), (133, 5493, 368), (20, 2209, 5888), (17, 2767, 4312),
          (661, 7659, 128), (665, 7429, 72), (4489, 133, 3584), (2734, 157, 5048), (2083, 5817, 192), (3877, 2081, 248), (285, 7411, 3200),
-         (137, 5471, 5896), (1709, 8131, 384), (2718, 4465, 328), (3796, 1061, 3392), (1181, 3567, 3256)]
+         (137, 5471, 5896), (1709, 8131, 384), (2718, 4465, 328), (3796, 1061, 3392), (1181, 3567, 3256),
+         (665, 5475, 4608), (1297, 3267, 4384), (16, 8192, 2048), (16, 1027, 16384), (48, 4099, 4096), (200, 2051, 4096)]
 TILES_GATED = [(259, 131, 64), (280, 129, 8), (24, 131, 6144), (21, 157, 5640), (72, 4291, 384), (69, 5105, 368), (18, 1725, 3904), (17, 1509, 4424),
                (661, 3917, 128), (484, 5299, 72), (130, 1851, 5120), (1878, 147, 5384), (836, 4761, 256), (668, 8191, 136), (141, 5733, 2432),
-               (154, 5473, 2448), (4283, 1417, 384), (1183, 5497, 328), (1207, 1669, 3648), (194, 5641, 5304)]
+               (154, 5473, 2448), (4283, 1417, 384), (1183, 5497, 328), (1207, 1669, 3648), (194, 5641, 5304), (201, 5773, 4560), (201, 5723, 5248),
+               (16, 4096, 8192), (45, 4099, 4096)]
 
 
 @pytest.mark.parametrize("T,N,K,gated", [(*s, False) for s in TILES] + [(*s, True) for s in TILES_GATED])
