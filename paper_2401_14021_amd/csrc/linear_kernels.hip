@@ -268,11 +268,11 @@ __device__ const uint4 zero_chunk = {0u, 0u, 0u, 0u};
 // 64 lanes x 16 bytes to 1 KB of LDS; not tracked by the compiler, waited for by count.  From a base and the lanes' 32-bit offsets, or from the lanes' own addresses.
 __device__ __forceinline__ void dma(const unsigned char *base, uint32_t voff, uint32_t lds_base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(base) : "memory");
+    asm volatile(RALM_M0_THEN "global_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(base) : "memory");
 }
 __device__ __forceinline__ void dma_at(const unsigned char *at, uint32_t lds_base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(at) : "memory");
+    asm volatile(RALM_M0_THEN "global_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(at) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_vmcnt()
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     }
     auto touch = [&](int strip) __attribute__((always_inline)) {
         const unsigned char *at = touch_base + (int64_t)(strip < KT ? strip : KT - 1) * 128;   // every strip begins inside the rows
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds0 + S * STAGE + wave * 256), "v"(touch_voff), "s"(at) : "memory");
+        asm volatile(RALM_M0_THEN "global_load_lds_dword %1, %2" ::"s"(lds0 + S * STAGE + wave * 256), "v"(touch_voff), "s"(at) : "memory");
     };
     auto next = [&]() __attribute__((always_inline)) {
         const int64_t step = !TOUCH && --until == 0 ? 128 - KT * 128 : 128;

@@ -16,6 +16,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// How a load into LDS begins that is written as inline asm; operand 0: its LDS address.  gfx9 asks for one wait state between a scalar write of M0 and such a load;
+// the compiler fills it in between instructions of its own, not inside an asm.
+#define RALM_M0_THEN "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+
 // ---- ranking keys -----------------------------------------------------------------------
 // A candidate (score, row id) is packed into one 64-bit key whose unsigned order is the
 // library's ranking: larger key = better = (higher score, then lower id).  -0.0 is folded

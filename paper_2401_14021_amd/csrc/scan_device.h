@@ -111,10 +111,10 @@ template <bool NT>
 __device__ __forceinline__ void dma_1kb(const unsigned char *base, uint32_t voff, uint32_t lds_base)
 {
     if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_base), "v"(voff), "s"(base)
+        asm volatile(RALM_M0_THEN "global_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_base), "v"(voff), "s"(base)
                      : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(base)
+        asm volatile(RALM_M0_THEN "global_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(base)
                      : "memory");
 }
 template <int N>
