@@ -16,9 +16,11 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// How a load into LDS begins that is written as inline asm; operand 0: its LDS address.  gfx9 asks for one wait state between a scalar write of M0 and such a load;
-// the compiler fills it in between instructions of its own, not inside an asm.
-#define RALM_M0_THEN "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+// How a load into LDS begins that is written as inline asm; operand 0: its LDS address.  gfx9 asks for one wait state between a scalar write of M0 and such a load, and for
+// five between a vector instruction that writes a scalar register and a load that takes its base from there: wherever the compiler has too few scalar registers, it
+// brings the base back by v_readlane right in front of the asm.  It fills in wait states between instructions of its own, not inside an asm: the move is one, the nop four
+// (against a nop of one: 8192^3 747 us and 750, 21 M rows x 1024 queries 25.8 ms and 25.7, x 256 queries 7.28 and 7.54).
+#define RALM_M0_THEN "s_mov_b32 m0, %0\n\ts_nop 3\n\t"
 
 // ---- ranking keys -----------------------------------------------------------------------
 // A candidate (score, row id) is packed into one 64-bit key whose unsigned order is the
