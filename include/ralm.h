@@ -693,7 +693,9 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
  *   w          device [N, K] of dtype ([2N, K] if gated), rows w_stride apart
  *   bias       device [N] ([2N]) of dtype, or NULL
  *   act        RALM_ACT_*; gelu is x Phi(x), gelu_tanh its usual approximation,
- *              silu x / (1 + exp(-x))
+ *              silu x / (1 + exp(-x)).  gelu is good to 2^-20 of its value where out is fp32, to
+ *              2^-17 before the rounding to 16 bits; silu and gelu_tanh, which are x / (1 + exp(e)),
+ *              to 2^-21 (1 + |e|) of theirs; all down to 2^-118
  *   residual   device [T, N] of out_dtype, or NULL; it may be out itself (same
  *              stride), and must not overlap it otherwise
  *   out        device [T, N] of out_dtype (dtype or fp32); must not overlap x, w or bias
