@@ -699,9 +699,11 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
  *   residual   device [T, N] of out_dtype, or NULL; it may be out itself (same
  *              stride), and must not overlap it otherwise
  *   out        device [T, N] of out_dtype (dtype or fp32); must not overlap x, w or bias
- *   workspace  ralm_linear_workspace_bytes(), 16-byte aligned (may be NULL where
- *              that is 0): sums of products that are split over workgroups.  Fewer rows are split further and
- *              may need more: one workspace for several T has the largest size of theirs
+ *   workspace  16-byte aligned, sums of products that are split over workgroups:
+ *              ralm_linear_workspace_bytes() of T or more rows, a search on the host (0.1 ms for 256 rows, 0.3 ms for 8192)
+ *              for what is enough for all calls of up to so many; or
+ *              ralm_linear_workspace_bytes_exact(), what a call of exactly T rows needs (fewer rows may need more).
+ *              May be NULL where that is 0
  *
  * Strides of 0 are dense.  K is a multiple of 8 in [8, 2^17]; x and w are 16-byte
  * aligned and their strides multiples of 8 elements, at most 2^22; out, residual
@@ -712,6 +714,7 @@ ralm_status ralm_verify_draft(const int32_t *draft_ids, const void *draft_probs,
  */
 enum { RALM_ACT_NONE = 0, RALM_ACT_RELU = 1, RALM_ACT_GELU = 2, RALM_ACT_GELU_TANH = 3, RALM_ACT_SILU = 4 };
 size_t ralm_linear_workspace_bytes(int64_t T, int32_t N, int32_t K, int32_t gated);
+size_t ralm_linear_workspace_bytes_exact(int64_t T, int32_t N, int32_t K, int32_t gated);
 ralm_status ralm_linear(const void *x, int64_t x_stride, int64_t T, const void *w, int64_t w_stride, int32_t N,
                         int32_t K, int32_t dtype, const void *bias, int32_t act, int32_t gated,
                         const void *residual, int64_t residual_stride, void *out, int64_t out_stride,

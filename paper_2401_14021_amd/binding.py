@@ -135,7 +135,7 @@ def lib() -> ctypes.CDLL:
         L.ralm_verify_draft_workspace_bytes.argtypes = [i64, i32]
         L.ralm_verify_draft.argtypes = [vp, vp, i64, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, size, vp]
         f32, f64 = ctypes.c_float, ctypes.c_double
-        L.ralm_linear_workspace_bytes.argtypes = [i64, i32, i32, i32]
+        L.ralm_linear_workspace_bytes.argtypes = L.ralm_linear_workspace_bytes_exact.argtypes = [i64, i32, i32, i32]
         L.ralm_linear.argtypes = [vp, i64, i64, vp, i64, i32, i32, i32, vp, i32, i32, vp, i64, vp, i64, i32, vp, size, vp]
         L.ralm_residual_norm.argtypes = [ctypes.POINTER(ralm_norm_t), vp]
         L.ralm_kv_append_rotary.argtypes = [kvp, i32, vp, i64, i64, i32, vp, i64, i64, vp, vp, i32, i64, i64, i64, i64, vp, i32, i32, f64, vp, vp,
@@ -146,7 +146,8 @@ def lib() -> ctypes.CDLL:
         for name in ("ralm_linear", "ralm_residual_norm", "ralm_kv_append_rotary", "ralm_rotary_frequencies", "ralm_knnlm_target"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("ralm_kv_page_bytes", "ralm_kv_attention_workspace_bytes", "ralm_kv_pages_workspace_bytes",
-                     "ralm_verify_draft_workspace_bytes", "ralm_linear_workspace_bytes", "ralm_knnlm_target_workspace_bytes"):
+                     "ralm_verify_draft_workspace_bytes", "ralm_linear_workspace_bytes", "ralm_linear_workspace_bytes_exact",
+                     "ralm_knnlm_target_workspace_bytes"):
             getattr(L, name).restype = size
         for name in ("ralm_kv_append", "ralm_kv_read", "ralm_kv_attention", "ralm_kv_reserve", "ralm_kv_fork", "ralm_kv_truncate",
                      "ralm_kv_copy_pages", "ralm_kv_compact", "ralm_verify_draft"):
@@ -707,7 +708,7 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 def alloc_linear_workspace(T: int, N: int, K: int, gated: bool = False, device="cuda") -> Optional[torch.Tensor]:
-    """For ralm_linear of T rows of these sizes (fewer may need more); None where none is needed."""
+    """For ralm_linear of up to T rows of these sizes; None where none is needed."""
     n = int(lib().ralm_linear_workspace_bytes(T, N, K, 1 if gated else 0))
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
@@ -737,7 +738,8 @@ def ralm_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] =
     out, os_ = _out_matrix(out, T, N, out_dtype, x.device)
     stream = _here(x, w, bias, residual, out, workspace)
     if workspace is None:
-        workspace = alloc_linear_workspace(T, N, K, gated, x.device)
+        n = int(lib().ralm_linear_workspace_bytes_exact(T, N, K, 1 if gated else 0))
+        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
     _check(lib().ralm_linear(x.data_ptr(), xs, T, w.data_ptr(), ws, N, K, _DT[x.dtype], _ptr(bias), ACTIVATIONS[act], 1 if gated else 0,
                              _ptr(residual), rs, out.data_ptr(), os_, _DT[out_dtype], _ptr(workspace),
                              0 if workspace is None else workspace.numel(), stream))

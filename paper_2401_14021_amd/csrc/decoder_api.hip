@@ -40,6 +40,11 @@ extern "C" {
 size_t ralm_linear_workspace_bytes(int64_t T, int32_t N, int32_t K, int32_t gated)
 {
     if (check_linear(T, N, K, gated) != RALM_OK || T == 0) return 0;
+    return (size_t)linear_most_sums(T, N, K, gated) * linear_plan(T, N, K, gated).pitch * 4;
+}
+size_t ralm_linear_workspace_bytes_exact(int64_t T, int32_t N, int32_t K, int32_t gated)
+{
+    if (check_linear(T, N, K, gated) != RALM_OK || T == 0) return 0;
     return sums_bytes(linear_plan(T, N, K, gated), T);
 }
 

@@ -30,7 +30,9 @@ struct LinearPlan {
     int64_t pitch;                // of the parts' sums, [parts][T][pitch]
     float *sums;
 };
+constexpr int64_t LINEAR_MAX_SUMS = 1LL << 31;   // numbers that a split depth leaves
 LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated);
+int64_t linear_most_sums(int64_t T, int32_t N, int32_t K, int32_t gated);   // parts x rows, of any number of rows up to T; 0: nothing is split
 hipError_t launch_linear(const LinearParams &p, const LinearPlan &plan, hipStream_t stream);
 
 hipError_t launch_residual_norm(const ralm_norm_t &p, hipStream_t stream);

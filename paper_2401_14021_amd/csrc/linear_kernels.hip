@@ -645,7 +645,10 @@ hipError_t launch_of(const LinearParams &p, const LinearPlan &plan, hipStream_t 
 // few MB).  Over these sizes the form that is taken is 1.2 % slower than the fastest one in the mean and 24 % at most (T 16, K 6144, N 2048: 14.6, 11.8 us).  What it
 // decides between, us: T 1, K = N = 1024: few 4.7, tiles 7.5; T 64, K 4096, N 6144: few 25, tiles of 128 x 64 in 4 parts 16.7; T 1387, K 4096, N 6144: tiles of
 // 128 x 128 100, of 256 x 192 74, of 256 x 256 85.
-LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
+//
+// consider(form, parts, us) for everything that may be taken
+template <class F>
+static void linear_candidates(int64_t T, int32_t N, int32_t K, int32_t gated, F consider)
 {
     struct Tile {
         int32_t form, bm, bn, per_cu;
@@ -661,13 +664,6 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
     const int64_t rows = (int64_t)N << gated;
     const int32_t strips = (K + 63) / 64;
     auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    LinearPlan plan;
-    float best = 0.f;
-    plan.form = -1;
-    plan.parts = 1;
-    auto consider = [&](int32_t form, int32_t parts, float t) {
-        if (plan.form < 0 || t < best) plan.form = form, plan.parts = parts, best = t;
-    };
     if (T <= 256) {
         static const float strip[] = {0.249f, 0.593f, 2.256f};   // of 16, 32, 64 weights
         for (int f = 0; f < 2; ++f) {
@@ -687,7 +683,7 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
         };
         for (int32_t parts : parts_of) {
             // at least two strips a part; sums of less than 2^31 numbers
-            if (parts > 1 && (strips / parts < 2 || T * rows > (1LL << 31) / parts)) break;
+            if (parts > 1 && (strips / parts < 2 || T * rows > LINEAR_MAX_SUMS / parts)) break;
             const int64_t wgs = all * parts, full = wgs / slots, rest = wgs - full * slots;
             const float n = (float)ceil_div(strips, parts);
             float t = 0.62f + (float)full * (n * strip(slots, tile.per_cu) + tile.epilogue);
@@ -696,11 +692,50 @@ LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
             consider(tile.form, parts, t);
         }
     }
+}
+
+LinearPlan linear_plan(int64_t T, int32_t N, int32_t K, int32_t gated)
+{
+    LinearPlan plan;
+    float best = 0.f;
+    plan.form = -1;
+    plan.parts = 1;
+    linear_candidates(T, N, K, gated, [&](int32_t form, int32_t parts, float t) {
+        if (plan.form < 0 || t < best) plan.form = form, plan.parts = parts, best = t;
+    });
+    const int32_t strips = (K + 63) / 64;
     plan.part_strips = (strips + plan.parts - 1) / plan.parts;
     plan.parts = (strips + plan.part_strips - 1) / plan.part_strips;   // none without a strip
     plan.pitch = (int64_t)((N + 3) / 4 * 4) << gated;
     plan.sums = nullptr;
     return plan;
+}
+
+// The most parts x rows that any call of up to T rows has.  From 257 rows on, 64 at a time: among them every form has the same tiles, and its time is a constant
+// plus parts x rows x another one for all forms.  So what is fastest for more of the rows has no more parts than what is for the first one, except that roundings of
+// fp32 may show where two are as fast; forms within 1e-5 of the fastest count as well.
+int64_t linear_most_sums(int64_t T, int32_t N, int32_t K, int32_t gated)
+{
+    int64_t most = 0;
+    for (int64_t t = 1; t <= T && t <= 256; ++t) {
+        const int32_t parts = linear_plan(t, N, K, gated).parts;
+        if (parts > 1 && parts * t > most) most = parts * t;
+    }
+    const int64_t rows = (int64_t)N << gated;
+    const int32_t strips = (K + 63) / 64;
+    for (int64_t t = 257; t <= T && t * rows <= LINEAR_MAX_SUMS / 2; t += 64) {
+        const int64_t last = T - t < 64 ? T : t + 63;
+        float best = 3.4e38f;
+        linear_candidates(t, N, K, gated, [&](int32_t, int32_t, float us) { best = fminf(best, us); });
+        int32_t parts = 1;
+        linear_candidates(t, N, K, gated, [&](int32_t, int32_t p, float us) {
+            if (us <= best * (1.f + 1e-5f) && p > parts) parts = p;
+        });
+        const int32_t each = (strips + parts - 1) / parts;
+        parts = (strips + each - 1) / each;
+        if (parts > 1 && parts * last > most) most = parts * last;
+    }
+    return most;
 }
 
 hipError_t launch_linear(const LinearParams &p, const LinearPlan &plan, hipStream_t stream)
