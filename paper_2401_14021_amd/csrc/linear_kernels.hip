@@ -377,7 +377,8 @@ __global__ __launch_bounds__(WM *WN * 64) void linear_tile_kernel(const LinearPa
     const int KT = strips - first < plan.part_strips ? strips - first : plan.part_strips;   // at least one
     const int tail = first + KT == strips ? p.K & 63 : 0;                                     // elements of the last strip, 0: all
     // Few rows, whose x an XCD's L2 holds: neighbouring tiles begin at other strips of their part and go round, or rows that lie a power of two apart would keep a few
-    // channels of the memory busy at a time (weights from HBM, us: T 16, K 16384, N 4096 in 8 parts 42, 30; T 45, K 4096, 22528 gated rows 48.6, 43.7)
+    // channels of the memory busy at a time (weights from HBM, us: T 16, K 16384, N 4096 in 8 parts 42, 30; T 45, K 4096, 22528 gated rows 48.6, 43.7).  A part of 13 strips begins at the same one in
+    // every tile, one of 26 at two, and the part that holds a broken strip at its first
     const int begin = !TOUCH && p.T * p.K <= 1 << 20 && !tail ? in / high * 13 % KT : 0;
     int until = KT - begin;
     wbase += (int64_t)(first + begin) * 128;

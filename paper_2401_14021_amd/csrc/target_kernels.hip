@@ -283,7 +283,8 @@ __device__ __forceinline__ const void *row_of(const void *p, int64_t at)
 __device__ __forceinline__ float share_of_model(float share, float sum) { return sum == 0.f ? 0.f : (1.f - share) / sum; }
 
 // Workgroups of 512 threads share a CU, so that a row's phases have others beside them: two of up to 128 registers, three where 16-bit entries are kept as they lie
-// (1300 rows of 32000, bf16 to fp32: a workgroup of 1024 threads, alone, 74, two 63, three 54 us, 4.6 TB/s; bf16 to bf16 55, 47.  Four spill: 68.  Shorter rows gain
+// (kernels alone, 1300 rows of 32000, bf16 to fp32: a workgroup of 1024 threads, alone, 74, two 63, three 54 us, 4.6 TB/s; bf16 to bf16 55, 47.  A stream of
+// calls, bf16 to fp32, takes 58 each.  Four spill: 68.  Shorter rows gain
 // nothing by it, and longer ones need 1024 threads' registers: 600 rows of 50257 52 us, packed 55.)
 template <int DT, int DO, int NT, int NV>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 512 && (NV == 8 || (NV == 16 && DT != DT_F32)) ? 6 : 4))) void target_row_kernel(const TargetParams p)
